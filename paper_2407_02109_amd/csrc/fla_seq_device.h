@@ -1,0 +1,135 @@
+// Device helpers shared by the kernels of fla_seq.h: 16-byte pieces of rows as fp32 values, and sums
+// and maxima over the lanes of a wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+namespace fla {
+
+typedef __bf16 bf16_t;
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+// 16, 8 and 4 bytes at any element's address (global memory takes them at any alignment)
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// values of a type in 16 bytes
+template <typename T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ float bits_f32(unsigned u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ unsigned f32_bits(float x) { return __builtin_bit_cast(unsigned, x); }
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+    const bf16x2_t p = {(bf16_t)a, (bf16_t)b};   // rounded to nearest even
+    return __builtin_bit_cast(unsigned, p);
+}
+
+// the first n values of a 16-byte piece at p (the others 0); n >= kVec: the whole piece
+__device__ __forceinline__ void load_piece(const float* p, int n, float (&v)[4]) {
+    if (n >= 4) {
+        const f32x4_any w = *reinterpret_cast<const f32x4_any*>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = w[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = j < n ? p[j] : 0.f;
+    }
+}
+__device__ __forceinline__ void unpack_piece(const u32x4_any& w, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = bits_f32(w[j] << 16);
+        v[2 * j + 1] = bits_f32(w[j] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load_piece(const bf16_t* p, int n, float (&v)[8]) {
+    if (n >= 8) {
+        unpack_piece(*reinterpret_cast<const u32x4_any*>(p), v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.f;
+    }
+}
+// eight fp32 values beside a piece of eight bf16
+__device__ __forceinline__ void load_piece(const float* p, int n, float (&v)[8]) {
+    float a[4], b[4];
+    load_piece(p, n, a);
+    load_piece(p + 4, n - 4, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = a[j];
+        v[4 + j] = b[j];
+    }
+}
+__device__ __forceinline__ void store_piece(float* p, int n, const float (&v)[4]) {
+    if (n >= 4) {
+        f32x4_any w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = v[j];
+        *reinterpret_cast<f32x4_any*>(p) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = v[j];
+    }
+}
+__device__ __forceinline__ void store_piece(bf16_t* p, int n, const float (&v)[8]) {
+    if (n >= 8) {
+        u32x4_any w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+        *reinterpret_cast<u32x4_any*>(p) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = (bf16_t)v[j];
+    }
+}
+
+// ---- over the lanes of a wave.  Lane permutations inside 16 lanes are operands of the vector ALU:
+//      with the lane's neighbour, its pair's, its quad's and its eight's mirror image.
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp(unsigned x) {
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+constexpr int kSwapPair = 0xB1, kSwapTwo = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+
+struct SumOp {
+    __device__ __forceinline__ static unsigned of(unsigned a, unsigned b) { return f32_bits(bits_f32(a) + bits_f32(b)); }
+};
+// the larger of two bit patterns of |x|: their order is that of the values, and a NaN is above all
+struct MaxOp {
+    __device__ __forceinline__ static unsigned of(unsigned a, unsigned b) { return a > b ? a : b; }
+};
+
+// over groups of `lanes` neighbouring lanes (4 .. 64, a power of two): every lane gets the result
+template <typename OP>
+__device__ __forceinline__ unsigned over_lanes(unsigned x, int lanes) {
+    x = OP::of(x, dpp<kSwapPair>(x));
+    x = OP::of(x, dpp<kSwapTwo>(x));
+    if (lanes >= 8) x = OP::of(x, dpp<kMirror8>(x));
+    if (lanes >= 16) x = OP::of(x, dpp<kMirror16>(x));
+    if (lanes >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = OP::of(r[0], r[1]);
+    }
+    if (lanes >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        x = OP::of(r[0], r[1]);
+    }
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x) { return bits_f32(over_lanes<SumOp>(f32_bits(x), 64)); }
+
+// ---- host side
+template <typename A>
+inline hipError_t launch(void (*kernel)(A), int64_t groups, int threads, const A& args, hipStream_t stream) {
+    A copy = args;
+    void* params[] = {&copy};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)groups), dim3((unsigned)threads), params,
+                           0, stream);
+}
+
+}  // namespace fla

@@ -1,0 +1,111 @@
+// Arguments and launchers shared by the C ABI of fla_seq.h and its kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "fla_swin_internal.h"   // FastDiv
+
+namespace fla {
+
+// ---- residual + root-mean-square norm (fla_rms_norm.hip)
+struct NormArgs {
+    const void* x;
+    const void* residual;    // NULL: none
+    const void* weight;
+    void* y;                 // T, or bytes of the 8-bit output
+    void* sum;               // NULL: not kept
+    float* rstd;             // NULL: not kept
+    float* scales;           // 8-bit output
+    int64_t x_stride, residual_stride;
+    int64_t rows;
+    int D;
+    int group;               // channels per scale, 0: one per row
+    int weight_f32;
+    float eps, inv_D;
+};
+hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, int cus, hipStream_t stream);
+hipError_t launch_norm_q8(const NormArgs& a, bool bf16, int cus, hipStream_t stream);
+
+struct NormBwdArgs {
+    const void* dy;
+    const void* s;
+    const void* weight;
+    const float* rstd;
+    const void* dsum;        // NULL: none
+    void* dx;
+    float* dweight;
+    float* ws;               // [blocks, D]: each block's share of dweight
+    int64_t dy_stride, s_stride, dsum_stride;
+    int64_t rows;
+    int D;
+    int weight_f32;
+    float inv_D;
+    int blocks;
+};
+constexpr int kNormBwdBlocks = 512;   // at most: two for each compute unit of the chip
+hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream);
+
+// ---- rotary positions (fla_rotary.hip)
+struct RotaryTensor {
+    const void* in;
+    void* out;               // == in: in place
+    int64_t in_batch, in_token, in_head, out_batch, out_token, out_head;
+};
+struct RotaryArgs {
+    RotaryTensor q, k;
+    const void* positions;
+    const double* freqs;
+    int64_t pos_batch, pos_token;
+    int pos64, axes;
+    int B, L, hq, heads;     // heads: of q and k
+    int d, rot;
+    int turn_pieces;         // 16-byte pieces (of both halves, where pairs lie apart) that turn, per head
+    int pieces;              // with those that are copied
+    int tokens;              // tokens of a workgroup's turn
+    int64_t n_tokens;        // B * L
+    float mscale, sign;      // sign: -1 turns back
+    FastDiv div_L, div_half, div_heads;
+};
+constexpr int kRotaryTable = 512;   // (cos, sin) of one turn: tokens * rot / 2 at most
+hipError_t launch_rotary(const RotaryArgs& a, bool bf16, bool interleaved, int cus, hipStream_t stream);
+
+// ---- gated linear recurrence (fla_gated_scan.hip)
+constexpr int kScanChunk = 128;     // tokens
+constexpr int kScanChannels = 64;   // of a column
+struct ScanInput {
+    const void* p;
+    int64_t batch, token;
+};
+struct ScanArgs {
+    ScanInput x, r, i;
+    const float* lam;
+    const float* h0;         // NULL: 0
+    const int* lengths;      // NULL: L
+    void* h;
+    float* h_last;           // NULL: not kept
+    float* states;           // [B, columns, chunks, 64]: the state that enters each chunk (NULL: not kept)
+    int B, L, D;
+    int columns, chunks;
+    float c;
+};
+struct ScanBwdArgs {
+    ScanInput x, r, i, dh;   // dh.p NULL: 0
+    const float* lam;
+    const float* states;
+    const int* lengths;
+    const float* d_last;     // NULL: 0
+    void* dx;
+    void* dr;
+    void* di;
+    float* dlam;
+    float* dh0;              // NULL: not wanted
+    float* shares;           // [rows, 64 columns]: shares of dlam
+    int B, L, D;
+    int columns, chunks;
+    float c;
+};
+hipError_t launch_scan_fwd(const ScanArgs& a, bool bf16, hipStream_t stream);
+hipError_t launch_scan_bwd(const ScanBwdArgs& a, bool bf16, hipStream_t stream);
+
+}  // namespace fla
