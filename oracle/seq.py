@@ -110,10 +110,12 @@ def gated_scan(x, r, i, lam, h0=None, lengths=None, c=8.0):
 
     Per step: z is off by 8 u z (rate, sigmoid, product), a by that and exp2's 2 u, u by 20 u (m^2 from the
     series or 1 - a^2 >= 0.22, its root, the gate, three products); twice that for the states' joining
-    over runs and chunks."""
+    over runs and chunks.  A run is reduced from zero and the state that enters it added afterwards, so
+    roundings are relative to the parts and not to their sum: they are counted against `mag`, the same
+    recurrence over absolute values, which is at least every such part."""
     B, L, D = x.shape
     h = np.zeros((B, D)) if h0 is None else h0.copy()
-    e = np.zeros((B, D))
+    e, mag = np.zeros((B, D)), np.abs(h)
     out, bound = np.zeros_like(x), np.zeros_like(x)
     _, _, z, a, _, u = _gates(x, r, i, lam, c)
     lens = np.full(B, L) if lengths is None else np.clip(lengths, 0, L)
@@ -121,14 +123,16 @@ def gated_scan(x, r, i, lam, h0=None, lengths=None, c=8.0):
         live = (t < lens)[:, None]
         with np.errstate(invalid="ignore"):
             nh = a[:, t] * h + u[:, t]
-            ne = a[:, t] * e + 2 * U * ((22 + 8 * z[:, t]) * np.abs(a[:, t] * h) + 20 * np.abs(u[:, t]))
-        h, e = np.where(live, nh, h), np.where(live, ne, e)
+            ne = a[:, t] * e + 2 * U * ((22 + 8 * z[:, t]) * a[:, t] * mag + 20 * np.abs(u[:, t]))
+            nm = a[:, t] * mag + np.abs(u[:, t])
+        h, e, mag = np.where(live, nh, h), np.where(live, ne, e), np.where(live, nm, mag)
         out[:, t], bound[:, t] = np.where(live, h, 0), np.where(live, e, 0)
     return out, h, bound, e + U * np.abs(h)
 
 
 def gated_scan_bwd(x, r, i, lam, h0, lengths, dh, d_last, c=8.0):
-    """(dx, dr, di, dlam, dh0) and a bound on each."""
+    """(dx, dr, di, dlam, dh0) and a bound on each (g's roundings counted as h's are, against the recurrence over
+    absolute values)."""
     B, L, D = x.shape
     gr, gi, z, a, m2, u = _gates(x, r, i, lam, c)
     h, _, eh, _ = gated_scan(x, r, i, lam, h0, lengths, c)
@@ -137,7 +141,7 @@ def gated_scan_bwd(x, r, i, lam, h0, lengths, dh, d_last, c=8.0):
     eprev = np.concatenate([np.zeros((B, 1, D)), eh[:, :-1]], 1)
     lens = np.full(B, L) if lengths is None else np.clip(lengths, 0, L)
     p = np.zeros((B, D)) if d_last is None else d_last.copy()
-    e = np.zeros((B, D))
+    e, mag = np.zeros((B, D)), np.abs(p)
     dx, dr, di = np.zeros_like(x), np.zeros_like(x), np.zeros_like(x)
     bx, br, bi = np.zeros_like(x), np.zeros_like(x), np.zeros_like(x)
     share, bshare, ashare = np.zeros(D), np.zeros(D), np.zeros(D)
@@ -146,7 +150,8 @@ def gated_scan_bwd(x, r, i, lam, h0, lengths, dh, d_last, c=8.0):
         zt, at, mt, ut = z[:, t], a[:, t], m2[:, t], u[:, t]
         with np.errstate(invalid="ignore", divide="ignore"):
             g = p + (0 if dh is None else dh[:, t])
-            eg = e + 2 * U * np.abs(g)
+            mag_g = mag + (0 if dh is None else np.abs(dh[:, t]))
+            eg = e + 2 * U * mag_g
             over = np.where(zt > 0, zt / mt, 0.5)
             t1, t2 = over * at * at * ut, zt * at * prev[:, t]
             el = g * (t1 - t2)
@@ -156,13 +161,14 @@ def gated_scan_bwd(x, r, i, lam, h0, lengths, dh, d_last, c=8.0):
             vals = (g * m * gi[:, t], el * (1 - gr[:, t]), g * ut * (1 - gi[:, t]), el)
             bounds = (eg * m * gi[:, t] + 24 * U * np.abs(g * m * gi[:, t]),
                       bl * (1 - gr[:, t]) + 12 * U * np.abs(el), eg * np.abs(ut) + 40 * U * np.abs(g * ut), bl)
-            np_, ne = at * g, at * eg + 2 * U * (22 + 8 * zt) * np.abs(at * g)
+            np_, ne = at * g, at * eg + 2 * U * (22 + 8 * zt) * at * mag_g
+            nm = at * mag_g
         for dst, v in zip((dx, dr, di, bx, br, bi), (*vals[:3], *bounds)):
             dst[:, t] = np.where(live, v, 0)
         share += np.where(live, vals[3], 0).sum(0)
         ashare += np.where(live, np.abs(vals[3]), 0).sum(0)
         bshare += np.where(live, bounds[3], 0).sum(0)
-        p, e = np.where(live, np_, p), np.where(live, ne, e)
+        p, e, mag = np.where(live, np_, p), np.where(live, ne, e), np.where(live, nm, mag)
     f = _sigmoid(lam) / np.logaddexp(0.0, lam)
     dlam = share * f
     # shares are added over runs, chunks and sequences: a few hundred additions at most

@@ -131,22 +131,23 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBwdArgs a) {
     float handed = a.d_last && c1 < a.D ? a.d_last[(int64_t)b * a.D + c1] : 0.f;   // (wave 1's)
     for (int k = a.chunks - 1; k >= 0; --k) {
         const int t0 = k * kScanChunk + seg * S;
-        float d[S][N], u[S][N], gi[S][N], z2[S][N], gg[S][N];
+        float d[S][N], u[S][N], gi[S][N], gr[S][N], gg[S][N];
         float zs[N], h[N], p[N];
 #pragma unroll
         for (int t = 0; t < S; ++t) {
             const bool live = t0 + t < len;
             const int m = live ? n : 0;
-            load_piece(row_of<T>(a.r, b, t0 + t) + ch, m, z2[t]);
+            load_piece(row_of<T>(a.r, b, t0 + t) + ch, m, gr[t]);
             load_piece(row_of<T>(a.i, b, t0 + t) + ch, m, gi[t]);
             load_piece(row_of<T>(a.x, b, t0 + t) + ch, m, u[t]);
             load_piece(row_of<T>(a.dh.p ? a.dh : a.x, b, t0 + t) + ch, a.dh.p ? m : 0, gg[t]);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                z2[t][j] = live ? s2[j] * sigmoid(z2[t][j]) : 0.f;
+                gr[t][j] = live ? sigmoid(gr[t][j]) : 0.f;
                 gi[t][j] = sigmoid(gi[t][j]);
-                d[t][j] = __builtin_amdgcn_exp2f(-z2[t][j]);
-                u[t][j] *= __builtin_amdgcn_sqrtf(one_minus_square(d[t][j], z2[t][j])) * gi[t][j];
+                const float z2 = s2[j] * gr[t][j];
+                d[t][j] = __builtin_amdgcn_exp2f(-z2);
+                u[t][j] *= __builtin_amdgcn_sqrtf(one_minus_square(d[t][j], z2)) * gi[t][j];
             }
         }
 #pragma unroll
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBwdArgs a) {
             zs[j] = h[j] = p[j] = 0.f;
 #pragma unroll
             for (int t = 0; t < S; ++t) {
-                zs[j] += z2[t][j];
+                zs[j] = __builtin_fmaf(s2[j], gr[t][j], zs[j]);
                 h[j] = __builtin_fmaf(d[t][j], h[j], u[t][j]);
                 p[j] = d[S - 1 - t][j] * (gg[S - 1 - t][j] + p[j]);
             }
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBwdArgs a) {
             float dx[N], dr[N], di[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float z = z2[t][j] * kLn2, m2 = one_minus_square(d[t][j], z2[t][j]);
+                const float z2 = s2[j] * gr[t][j], z = z2 * kLn2, m2 = one_minus_square(d[t][j], z2);
                 const float v = gg[t][j] * u[t][j];
                 // z / m^2 -> 1/2 as z -> 0, where u is 0 too
                 const float over = z > 1e-30f ? z * __builtin_amdgcn_rcpf(m2) : 0.5f;
@@ -202,8 +203,7 @@ __global__ __launch_bounds__(256) void scan_bwd(ScanBwdArgs a) {
                 h[j] = __builtin_fmaf(d[t][j], h[j], u[t][j]);
                 dx[j] = gg[t][j] * __builtin_amdgcn_sqrtf(m2) * gi[t][j];
                 di[j] = v * (1.f - gi[t][j]);
-                // 1 - sigmoid(r) = 1 - z / rate
-                dr[j] = e * (1.f - (s2[j] > 0.f ? z2[t][j] * __builtin_amdgcn_rcpf(s2[j]) : 0.f));
+                dr[j] = e * (1.f - gr[t][j]);
                 esum[j] += e;
             }
             if (t0 + t < a.L) {
