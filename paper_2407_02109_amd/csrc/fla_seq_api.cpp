@@ -179,8 +179,9 @@ bool scan_too_large(int B, int L, int D) {
 int64_t scan_states_bytes(int B, int L, int D) {
     return (int64_t)B * scan_columns(D) * scan_chunks(L) * fla::kScanChannels * 4;
 }
-int64_t scan_ws_bytes(int, int, int) { return 0; }
-int64_t scan_bwd_ws_bytes(int B, int, int D) { return (int64_t)B * scan_columns(D) * fla::kScanChannels * 4; }
+int64_t scan_ws_bytes(int B, int L, int D) { return fla::scan_chain_bytes(B * scan_columns(D), scan_chunks(L)); }
+// the chain's words and the chunks' shares of dlam
+int64_t scan_bwd_ws_bytes(int B, int L, int D) { return scan_ws_bytes(B, L, D) + scan_states_bytes(B, L, D); }
 
 int scan_bytes(int B, int L, int D, size_t* bytes, int64_t (*of)(int, int, int)) {
     const int st = scan_sizes(B, L, D);
@@ -434,6 +435,7 @@ int fla_gated_scan_fwd(const void* x, int64_t x_batch, int64_t x_token, const vo
     a.h = h;
     a.h_last = h_last;
     a.states = states;
+    a.ws = workspace;
     a.B = B;
     a.L = L;
     a.D = D;
@@ -497,7 +499,8 @@ int fla_gated_scan_bwd(const void* x, int64_t x_batch, int64_t x_token, const vo
     a.di = di;
     a.dlam = dlam;
     a.dh0 = dh0;
-    a.shares = static_cast<float*>(workspace);
+    a.ws = workspace;
+    a.shares = reinterpret_cast<float*>(static_cast<char*>(workspace) + scan_ws_bytes(B, L, D));
     a.B = B;
     a.L = L;
     a.D = D;

@@ -85,6 +85,7 @@ struct ScanArgs {
     void* h;
     float* h_last;           // NULL: not kept
     float* states;           // [B, columns, chunks, 64]: the state that enters each chunk (NULL: not kept)
+    void* ws;                // the chain's words (several chunks)
     int B, L, D;
     int columns, chunks;
     float c;
@@ -100,11 +101,18 @@ struct ScanBwdArgs {
     void* di;
     float* dlam;
     float* dh0;              // NULL: not wanted
-    float* shares;           // [rows, 64 columns]: shares of dlam
+    void* ws;                // the chain's words (several chunks)
+    float* shares;           // [B, columns, chunks, 64]: shares of dlam
     int B, L, D;
     int columns, chunks;
     float c;
 };
+// The chain's words: for each (column, chunk, channel) 12 bytes, then a ticket for each column, in cache lines of
+// their own.
+constexpr int kScanTicketWords = 32;
+inline int64_t scan_chain_bytes(int64_t columns, int64_t chunks) {
+    return chunks > 1 ? columns * (chunks * kScanChannels * 12 + kScanTicketWords * 4) : 0;
+}
 hipError_t launch_scan_fwd(const ScanArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_scan_bwd(const ScanBwdArgs& a, bool bf16, hipStream_t stream);
 
