@@ -16,26 +16,30 @@
 // The state that enters a chunk comes from the chunk before it, in one pass over the data: as soon as a
 // workgroup has its chunk's decay A and state from zero H, it publishes both, then looks back over the
 // chunks before it for the nearest one whose outgoing state is known, runs A and H of those between
-// over it, and publishes its own outgoing state.  The values are their own flags: a word is all ones
-// until it is published, and no value has that pattern.  The states meet in chunk order whatever is found
-// first, so the result does not depend on timing.  Workgroups draw the chunks of a column in order, so
+// over it, and publishes its own outgoing state.  The states meet in chunk order whatever is found first, so the
+// result does not depend on timing.  Workgroups draw the chunks of a column in order, so
 // a workgroup waits only for ones that have begun, and the first of a column waits for none: every
 // wait ends.
 #include "fla_seq_device.h"
 #include "fla_seq_internal.h"
+
+#include <type_traits>
 
 namespace fla {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-template <typename T, int THREADS>
+// A tile of CHUNK tokens in a workgroup of THREADS.
+template <typename T, int CHUNK, int THREADS>
 struct Tile {
     static constexpr int N = kVec<T>;                // channels of a thread
     static constexpr int X = kScanChannels / N;      // threads across the column
     static constexpr int SEG = THREADS / X;          // runs of tokens
-    static constexpr int S = kScanChunk / SEG;       // tokens of a run
+    static constexpr int S = CHUNK / SEG;            // tokens of a run
+    static constexpr int WAVES = THREADS / 64;
 };
+constexpr int kBwdThreads = 512;
 
 __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e));
@@ -44,16 +48,17 @@ __device__ __forceinline__ float sigmoid(float v) {
 __device__ __forceinline__ float decay_rate(float lam, float c) {
     return c * kLog2e * (fmaxf(lam, 0.f) + log1pf(expf(-fabsf(lam))));
 }
-// 1 - a^2 for a = 2^-z2: near a = 1 from the series of 1 - exp(-w), w = 2 z2 ln 2, whose first dropped term is
-// w^6 / 5040 (5e-8 at w = 1/4); there 1 - a^2 in fp32 would lose what a's rounding takes
+// 1 - a^2 for a = 2^-z2: near a = 1 from the series of 1 - exp(-w), w = 2 z2 ln 2, in powers of z2; its first dropped
+// term is w^6 / 5040 of the value (5e-8 at w = 1/4).  There 1 - a^2 in fp32 would lose what a's rounding takes.
 __device__ __forceinline__ float one_minus_square(float a, float z2) {
-    const float w = z2 * (2.f * kLn2);
-    float p = __builtin_fmaf(w, -1.f / 6.f, 1.f);
-    p = __builtin_fmaf(w * p, -1.f / 5.f, 1.f);
-    p = __builtin_fmaf(w * p, -1.f / 4.f, 1.f);
-    p = __builtin_fmaf(w * p, -1.f / 3.f, 1.f);
-    p = __builtin_fmaf(w * p, -1.f / 2.f, 1.f);
-    return w < 0.25f ? w * p : __builtin_fmaf(-a, a, 1.f);
+    constexpr float w = 2.f * kLn2;
+    float p = __builtin_fmaf(z2, -w * w * w * w * w * w / 720.f, w * w * w * w * w / 120.f);
+    p = __builtin_fmaf(z2, p, -w * w * w * w / 24.f);
+    p = __builtin_fmaf(z2, p, w * w * w / 6.f);
+    p = __builtin_fmaf(z2, p, -w * w / 2.f);
+    p = __builtin_fmaf(z2, p, w) * z2;
+    const float q = __builtin_fmaf(-a, a, 1.f);
+    return z2 < 0.25f / w ? p : q;
 }
 
 // tokens of sequence b
@@ -116,169 +121,241 @@ __global__ __launch_bounds__(256) void scan_serial(ScanArgs a) {
     }
 }
 
-// ---- the chain over the chunks of a column.  Words of the workspace, all ones until published:
-//      for each (column, chunk, channel) A and H in one 64-bit word, and the outgoing state.
+// ---- the chain over the chunks of a column, in the order in which it runs ("links").  Words of the workspace, all
+//      ones until published: for each (column, link, channel) A and H in one 64-bit word, and the outgoing
+//      state.  And a mark for each link: 1 with A and H, 2 with the outgoing state, so that one load of 64 marks
+//      shows how far back to go; the words tell for themselves whether they are there.
 struct Chain {
-    unsigned long long* part;   // [chunks][64] of this column, in the order in which the chain runs
-    unsigned* out;
+    unsigned long long* part;   // [links][64] of this column
+    unsigned* out;              // [links][64]
+    unsigned* mark;             // [links]
+    unsigned* ticket;
 };
-__device__ __forceinline__ Chain chain_of(void* ws, int64_t columns, int chunks, int64_t column) {
-    const int64_t all = columns * chunks * kScanChannels, mine = column * chunks * kScanChannels;
+__device__ __forceinline__ Chain chain_of(void* ws, int64_t columns, int links, int64_t column) {
+    const int64_t all = columns * links, mine = column * links;
     Chain c;
-    c.part = static_cast<unsigned long long*>(ws) + mine;
-    c.out = reinterpret_cast<unsigned*>(static_cast<unsigned long long*>(ws) + all) + mine;
+    c.part = static_cast<unsigned long long*>(ws) + mine * kScanChannels;
+    unsigned* w = reinterpret_cast<unsigned*>(static_cast<unsigned long long*>(ws) + all * kScanChannels);
+    c.out = w + mine * kScanChannels;
+    w += all * kScanChannels;
+    c.mark = w + mine;
+    c.ticket = w + all + column * kScanTicketWords;
     return c;
 }
-// the next chunk of the column, in order (one draw a workgroup)
-__device__ __forceinline__ unsigned draw(void* ws, int64_t columns, int chunks, int64_t column) {
-    unsigned* tickets = reinterpret_cast<unsigned*>(static_cast<unsigned char*>(ws) +
-                                                    columns * chunks * kScanChannels * 12);
-    return __scoped_atomic_fetch_add(tickets + column * kScanTicketWords, 1u, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+template <typename W>
+__device__ __forceinline__ W seen(const W* p) {
+    return __scoped_atomic_load_n(p, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+}
+template <typename W>
+__device__ __forceinline__ void put(W* p, W v) {
+    __scoped_atomic_store_n(p, v, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+}
+// the next link of the column, in order (one draw a workgroup)
+__device__ __forceinline__ int draw(const Chain& c) {
+    return (int)__scoped_atomic_fetch_add(c.ticket, 1u, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
 }
 constexpr unsigned kUnset = 0xffffffffu;
 __device__ __forceinline__ unsigned word_of(float v) {
     const unsigned u = f32_bits(v);
     return u == kUnset ? 0x7fc00000u : u;   // (that NaN becomes another)
 }
-__device__ __forceinline__ void publish(const Chain& c, int k, int lane, float v) {
-    __scoped_atomic_store_n(c.out + k * kScanChannels + lane, word_of(v), __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+__device__ __forceinline__ void publish(const Chain& c, int link, int lane, float v) {
+    put(c.out + (int64_t)link * kScanChannels + lane, word_of(v));
+    if (lane == 0) put(c.mark + link, 2u);
 }
-__device__ __forceinline__ void publish(const Chain& c, int k, int lane, float A, float H) {
-    __scoped_atomic_store_n(c.part + k * kScanChannels + lane,
-                            (unsigned long long)word_of(A) << 32 | word_of(H), __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
+__device__ __forceinline__ void publish(const Chain& c, int link, int lane, float A, float H) {
+    put(c.part + (int64_t)link * kScanChannels + lane, (unsigned long long)word_of(A) << 32 | word_of(H));
+    if (lane == 0) put(c.mark + link, 1u);
 }
-// The outgoing state of link k - 1, for one wave (a lane each channel).  A turn reads kLook links; a lane has
-// its state once an outgoing state and the parts of all links behind it are there.
-constexpr int kLook = 8;
+// The outgoing state of link - 1, for one wave (a lane each channel): the nearest outgoing state, and A and H of the
+// links behind it over it, in order.
 constexpr int kMostTurns = 1 << 22;   // seconds: only a workspace that another call overwrites makes a wait that long
-__device__ __forceinline__ float look_back(const Chain& c, int k, int lane) {
-    float state = 0.f;
-    bool found = false;
+__device__ __forceinline__ float look_back(const Chain& c, int link, int lane) {
+    constexpr int kBatch = 8;
     for (int turn = 0; turn < kMostTurns; ++turn) {
-        if (!found) {
-            unsigned out[kLook];
-            unsigned long long part[kLook];
+        const unsigned m = lane < link ? seen(c.mark + (link - 1 - lane)) : 0u;
+        const unsigned long long outs = __builtin_amdgcn_ballot_w64(m == 2u), parts = __builtin_amdgcn_ballot_w64(m != 0u);
+        if (outs != 0) {
+            const int near = __builtin_ctzll(outs);   // links behind the nearest outgoing state
+            const unsigned long long behind = (1ull << near) - 1;
+            if ((parts & behind) == behind) {
+                const int first = link - 1 - near;
+                const unsigned w = seen(c.out + (int64_t)first * kScanChannels + lane);
+                bool there = true;
+                float state = bits_f32(w);
+                for (int at = first + 1; at < link; at += kBatch) {
+                    // (a batch is asked for at once, without a condition, past the last link that one again)
+                    unsigned long long p[kBatch];
 #pragma unroll
-            for (int i = 0; i < kLook; ++i) {
-                const int at = (k - 1 - i > 0 ? k - 1 - i : 0) * kScanChannels + lane;
-                out[i] = __scoped_atomic_load_n(c.out + at, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
-                part[i] = __scoped_atomic_load_n(c.part + at, __ATOMIC_RELAXED, __MEMORY_SCOPE_DEVICE);
-            }
-            // the nearest outgoing state with every part behind it
-            int near = -1;
-            bool parts = true;
+                    for (int i = 0; i < kBatch; ++i)
+                        p[i] = seen(c.part + (int64_t)(at + i < link ? at + i : link - 1) * kScanChannels + lane);
 #pragma unroll
-            for (int i = 0; i < kLook; ++i) {
-                if (near < 0 && parts && i < k && out[i] != kUnset) near = i;
-                parts = parts && part[i] != ~0ull;
-            }
-            if (near >= 0) {
-                found = true;
-#pragma unroll
-                for (int i = kLook - 1; i >= 0; --i) {
-                    if (i == near) state = bits_f32(out[i]);
-                    if (i < near)
-                        state = __builtin_fmaf(bits_f32((unsigned)(part[i] >> 32)), state, bits_f32((unsigned)part[i]));
+                    for (int i = 0; i < kBatch; ++i)
+                        if (at + i < link) {
+                            there = there && p[i] != ~0ull;
+                            state = __builtin_fmaf(bits_f32((unsigned)(p[i] >> 32)), state, bits_f32((unsigned)p[i]));
+                        }
                 }
+                there = there && w != kUnset;
+                if (__builtin_amdgcn_ballot_w64(!there) == 0) return state;
             }
         }
-        if (__builtin_amdgcn_ballot_w64(!found) == 0) return state;
         __builtin_amdgcn_s_sleep(1);
     }
-    return found ? state : __builtin_nanf("");
+    return __builtin_nanf("");
 }
 
-// the words of a workspace before a chain: all ones, and the tickets 0
+// the words of a workspace before a chain: all ones; the marks and tickets 0
 template <typename A>
 __global__ __launch_bounds__(256) void chain_clear(A a) {
     unsigned* ws = static_cast<unsigned*>(a.ws);
-    const int64_t columns = (int64_t)a.B * a.columns, words = columns * a.chunks * kScanChannels * 3;
-    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < words + columns * kScanTicketWords;
+    const int64_t columns = (int64_t)a.B * a.columns, words = columns * a.links * kScanChannels * 3;
+    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < words + columns * (a.links + kScanTicketWords);
          w += (int64_t)gridDim.x * 256)
         ws[w] = w < words ? kUnset : 0u;
 }
 
-template <typename T, bool CHAIN>
-__global__ __launch_bounds__(256) void scan_tiles(ScanArgs a) {
-    using Ti = Tile<T, 256>;
-    constexpr int N = Ti::N, X = Ti::X, SEG = Ti::SEG, S = Ti::S;
-    // of each run: its decay and its state from zero; then the state that enters it
-    __shared__ float run_a[SEG][kScanChannels], run_h[SEG][kScanChannels];
+// Runs of one column and their joining.  The runs of a wave are neighbours, and a lane takes a channel of
+// them: it reduces the wave's runs to one, and once the state that enters the wave is known, runs over
+// them again.  Only the waves' sums cross the workgroup.
+template <int SEG, int WAVES>
+struct Runs {
+    static constexpr int PER = SEG / WAVES;   // runs of a wave
+    float a[SEG][kScanChannels];              // decay of each run
+    float h[SEG][kScanChannels];              // its state from zero; then the state that enters it
+    float wave_a[WAVES][kScanChannels], wave_h[WAVES][kScanChannels];   // the same of a wave's runs
+};
+// the order of LDS accesses within a wave is theirs in the program
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// runs [s0, s0 + PER) in order (BACK: from the last) to one, in (A, H)
+template <int PER, bool BACK>
+__device__ __forceinline__ void join(const float (*ra)[kScanChannels], const float (*rh)[kScanChannels], int s0, int lane,
+                                     float& A, float& H) {
+    A = 1.f;
+    H = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = s0 + (BACK ? PER - 1 - i : i);
+        H = __builtin_fmaf(ra[s][lane], H, rh[s][lane]);
+        A *= ra[s][lane];
+    }
+}
+// the states that enter the runs, from the one that enters the first, in place of rh
+template <int PER, bool BACK>
+__device__ __forceinline__ float enter(const float (*ra)[kScanChannels], float (*rh)[kScanChannels], int s0, int lane,
+                                       float st) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = s0 + (BACK ? PER - 1 - i : i);
+        const float next = __builtin_fmaf(ra[s][lane], st, rh[s][lane]);
+        rh[s][lane] = st;
+        st = next;
+    }
+    return st;
+}
+
+// (32 values a thread; four waves on a SIMD)
+template <typename T, int CHUNK, bool CHAIN>
+__global__ __launch_bounds__(2 * CHUNK, 4) void scan_tiles(ScanArgs a) {
+    using Ti = Tile<T, CHUNK, 2 * CHUNK>;
+    constexpr int N = Ti::N, X = Ti::X, SEG = Ti::SEG, S = Ti::S, WAVES = Ti::WAVES;
+    using R = Runs<SEG, WAVES>;
+    __shared__ R runs;
     __shared__ float rate[kScanChannels];
     __shared__ int drawn;
-    const int tid = (int)threadIdx.x, seg = tid / X, lc = tid % X * N;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = tid / X, lc = tid % X * N;
     const unsigned columns = (unsigned)(a.B * a.columns), column = blockIdx.x % columns;
     const int g = (int)(column % (unsigned)a.columns), b = (int)(column / (unsigned)a.columns);
     const int ch = g * kScanChannels + lc, n = a.D - ch;
-    const int c1 = g * kScanChannels + (tid & 63);   // the carrying wave's channel
-    if (CHAIN && tid == 0) drawn = (int)draw(a.ws, columns, a.chunks, column);
+    const int c1 = g * kScanChannels + lane;   // the channel of a joining lane
+    if (CHAIN && tid == 0) drawn = draw(chain_of(a.ws, columns, a.links, column));
     if (tid < 64) rate[tid] = c1 < a.D ? decay_rate(a.lam[c1], a.c) : 0.f;
     __syncthreads();
     const int k = CHAIN ? drawn : 0;
     const int len = length_of(a.lengths, b, a.L);
-    const int t0 = k * kScanChunk + seg * S;
-    float d[S][N], u[S][N], gi[S][N];
-#pragma unroll
-    for (int t = 0; t < S; ++t) {
-        const int m = t0 + t < len ? n : 0;
-        load_piece(row_of<T>(a.r, b, t0 + t) + ch, m, d[t]);
-        load_piece(row_of<T>(a.i, b, t0 + t) + ch, m, gi[t]);
-        load_piece(row_of<T>(a.x, b, t0 + t) + ch, m, u[t]);
-    }
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const float s2 = rate[lc + j];
-        float zs = 0.f, h = 0.f;
+    const int t0 = k * CHUNK + seg * S;
+    float d[S][N], u[S][N];
+    // WHOLE: every token and channel of the tile is there
+    auto load = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        float gi[S][N];
 #pragma unroll
         for (int t = 0; t < S; ++t) {
-            const float z2 = t0 + t < len ? s2 * sigmoid(d[t][j]) : 0.f;
-            d[t][j] = __builtin_amdgcn_exp2f(-z2);
-            u[t][j] *= __builtin_amdgcn_sqrtf(one_minus_square(d[t][j], z2)) * sigmoid(gi[t][j]);
-            zs += z2;
-            h = __builtin_fmaf(d[t][j], h, u[t][j]);
+            const int m = WHOLE ? N : t0 + t < len ? n : 0;
+            load_piece(row_of<T>(a.r, b, t0 + t) + ch, m, d[t]);
+            load_piece(row_of<T>(a.i, b, t0 + t) + ch, m, gi[t]);
+            load_piece(row_of<T>(a.x, b, t0 + t) + ch, m, u[t]);
         }
-        run_a[seg][lc + j] = __builtin_amdgcn_exp2f(-zs);
-        run_h[seg][lc + j] = h;
-    }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float s2 = rate[lc + j];
+            float zs = 0.f, h = 0.f;
+#pragma unroll
+            for (int t = 0; t < S; ++t) {
+                const float z2 = WHOLE || t0 + t < len ? s2 * sigmoid(d[t][j]) : 0.f;
+                d[t][j] = __builtin_amdgcn_exp2f(-z2);
+                u[t][j] *= __builtin_amdgcn_sqrtf(one_minus_square(d[t][j], z2)) * sigmoid(gi[t][j]);
+                zs += z2;
+                h = __builtin_fmaf(d[t][j], h, u[t][j]);
+            }
+            runs.a[seg][lc + j] = __builtin_amdgcn_exp2f(-zs);
+            runs.h[seg][lc + j] = h;
+        }
+    };
+    const bool whole = (int64_t)(k + 1) * CHUNK <= len && (g + 1) * kScanChannels <= a.D;
+    if (whole)
+        load(std::true_type{});
+    else
+        load(std::false_type{});
+    wave_order();
+    float A, H;
+    join<R::PER, false>(runs.a, runs.h, wave * R::PER, lane, A, H);
+    runs.wave_a[wave][lane] = A;
+    runs.wave_h[wave][lane] = H;
     __syncthreads();
-    if (tid < 64) {
+    if (wave == 0) {
         float st = 0.f;
         if (k == 0) {
             if (a.h0 && c1 < a.D) st = a.h0[(int64_t)b * a.D + c1];
             if (a.h_last && len == 0 && c1 < a.D) a.h_last[(int64_t)b * a.D + c1] = st;
         }
         if constexpr (CHAIN) {
-            const Chain c = chain_of(a.ws, columns, a.chunks, column);
-            float A = 1.f, H = 0.f;
-#pragma unroll 8
-            for (int s = 0; s < SEG; ++s) {
-                H = __builtin_fmaf(run_a[s][tid], H, run_h[s][tid]);
-                A *= run_a[s][tid];
-            }
+            const Chain c = chain_of(a.ws, columns, a.links, column);
+            join<WAVES, false>(runs.wave_a, runs.wave_h, 0, lane, A, H);
             if (k > 0) {
-                publish(c, k, tid, A, H);
-                st = look_back(c, k, tid);
+                publish(c, k, lane, A, H);
+                st = look_back(c, k, lane);
             }
-            publish(c, k, tid, __builtin_fmaf(A, st, H));
+            publish(c, k, lane, __builtin_fmaf(A, st, H));
         }
-        if (a.states) a.states[((int64_t)column * a.chunks + k) * kScanChannels + tid] = st;
-#pragma unroll 8
-        for (int s = 0; s < SEG; ++s) {
-            const float next = __builtin_fmaf(run_a[s][tid], st, run_h[s][tid]);
-            run_h[s][tid] = st;
-            st = next;
-        }
+        enter<WAVES, false>(runs.wave_a, runs.wave_h, 0, lane, st);
+        if (a.states)
+#pragma unroll
+            for (int q = 0; q < CHUNK / kScanChunk; ++q)
+                if (k * (CHUNK / kScanChunk) + q < a.chunks)
+                    a.states[((int64_t)column * a.chunks + k * (CHUNK / kScanChunk) + q) * kScanChannels + lane] =
+                        runs.wave_h[q * WAVES / (CHUNK / kScanChunk)][lane];
     }
     __syncthreads();
+    enter<R::PER, false>(runs.a, runs.h, wave * R::PER, lane, runs.wave_h[wave][lane]);
+    wave_order();
     float h[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) h[j] = run_h[seg][lc + j];
+    for (int j = 0; j < N; ++j) h[j] = runs.h[seg][lc + j];
 #pragma unroll
     for (int t = 0; t < S; ++t) {
-        if (t0 + t >= len) break;
+        if (!whole && t0 + t >= len) break;
 #pragma unroll
         for (int j = 0; j < N; ++j) h[j] = __builtin_fmaf(d[t][j], h[j], u[t][j]);
-        store_piece(static_cast<T*>(a.h) + ((int64_t)b * a.L + t0 + t) * a.D + ch, n, h);
+        T* row = static_cast<T*>(a.h) + ((int64_t)b * a.L + t0 + t) * a.D + ch;
+        if (whole)
+            store_piece(row, N, h);
+        else
+            store_piece(row, n, h);
         if (a.h_last && t0 + t == len - 1) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
@@ -290,116 +367,111 @@ __global__ __launch_bounds__(256) void scan_tiles(ScanArgs a) {
 // Backward: the chain runs from the last chunk to the first, over what a chunk hands on: q from zero, its decay
 // the forward's.  The states that enter the chunks are the forward's, kept.
 template <typename T>
-__global__ __launch_bounds__(512) void scan_bwd(ScanBwdArgs a) {
-    using Ti = Tile<T, 512>;
-    constexpr int N = Ti::N, X = Ti::X, SEG = Ti::SEG, S = Ti::S;
-    // of each run: its decay, its state from zero and what it hands on from zero; then the state that
-    // enters it and what it is handed
-    __shared__ float run_a[SEG][kScanChannels], run_h[SEG][kScanChannels], run_p[SEG][kScanChannels];
+__global__ __launch_bounds__(kBwdThreads, 4) void scan_bwd(ScanBwdArgs a) {
+    using Ti = Tile<T, kScanChunk, kBwdThreads>;
+    constexpr int N = Ti::N, X = Ti::X, SEG = Ti::SEG, S = Ti::S, WAVES = Ti::WAVES;
+    using R = Runs<SEG, WAVES>;
+    __shared__ R runs;
+    __shared__ float run_p[SEG][kScanChannels];   // what a run hands on from zero; then what it is handed
+    __shared__ float wave_p[WAVES][kScanChannels], wave_b[WAVES][kScanChannels];
     __shared__ float rate[kScanChannels];
     __shared__ int drawn;
-    const int tid = (int)threadIdx.x, seg = tid / X, lc = tid % X * N;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = tid / X, lc = tid % X * N;
     const unsigned columns = (unsigned)(a.B * a.columns), column = blockIdx.x % columns;
     const int g = (int)(column % (unsigned)a.columns), b = (int)(column / (unsigned)a.columns);
     const int ch = g * kScanChannels + lc, n = a.D - ch;
-    const int c1 = g * kScanChannels + (tid & 63);   // the carrying waves' channel
-    if (tid == 0) drawn = a.chunks > 1 ? (int)draw(a.ws, columns, a.chunks, column) : 0;
+    const int c1 = g * kScanChannels + lane;   // the channel of a joining lane
+    if (tid == 0) drawn = a.chunks > 1 ? draw(chain_of(a.ws, columns, a.links, column)) : 0;
     if (tid < 64) rate[tid] = c1 < a.D ? decay_rate(a.lam[c1], a.c) : 0.f;
     __syncthreads();
     const int link = drawn, k = a.chunks - 1 - link;
     const int len = length_of(a.lengths, b, a.L);
     const int t0 = k * kScanChunk + seg * S;
     float d[S][N], u[S][N], gi[S][N], gr[S][N], gg[S][N];
-#pragma unroll
-    for (int t = 0; t < S; ++t) {
-        const int m = t0 + t < len ? n : 0;
-        load_piece(row_of<T>(a.r, b, t0 + t) + ch, m, gr[t]);
-        load_piece(row_of<T>(a.i, b, t0 + t) + ch, m, gi[t]);
-        load_piece(row_of<T>(a.x, b, t0 + t) + ch, m, u[t]);
-        load_piece(row_of<T>(a.dh.p ? a.dh : a.x, b, t0 + t) + ch, a.dh.p ? m : 0, gg[t]);
-    }
-    float s2[N], h[N], p[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        float zs = 0.f;
-        s2[j] = rate[lc + j];
-        h[j] = p[j] = 0.f;
+    const bool whole = (int64_t)(k + 1) * kScanChunk <= len && (g + 1) * kScanChannels <= a.D;
+    auto load = [&](auto is_whole) {
+        constexpr bool WHOLE = decltype(is_whole)::value;
 #pragma unroll
         for (int t = 0; t < S; ++t) {
-            gr[t][j] = t0 + t < len ? sigmoid(gr[t][j]) : 0.f;
-            gi[t][j] = sigmoid(gi[t][j]);
-            const float z2 = s2[j] * gr[t][j];
-            d[t][j] = __builtin_amdgcn_exp2f(-z2);
-            u[t][j] *= __builtin_amdgcn_sqrtf(one_minus_square(d[t][j], z2)) * gi[t][j];
-            zs += z2;
-            h[j] = __builtin_fmaf(d[t][j], h[j], u[t][j]);
+            const int m = WHOLE ? N : t0 + t < len ? n : 0;
+            load_piece(row_of<T>(a.r, b, t0 + t) + ch, m, gr[t]);
+            load_piece(row_of<T>(a.i, b, t0 + t) + ch, m, gi[t]);
+            load_piece(row_of<T>(a.x, b, t0 + t) + ch, m, u[t]);
+            load_piece(row_of<T>(a.dh.p ? a.dh : a.x, b, t0 + t) + ch, a.dh.p ? m : 0, gg[t]);
         }
 #pragma unroll
-        for (int t = S - 1; t >= 0; --t) p[j] = d[t][j] * (gg[t][j] + p[j]);
-        run_a[seg][lc + j] = __builtin_amdgcn_exp2f(-zs);
-        run_h[seg][lc + j] = h[j];
-        run_p[seg][lc + j] = p[j];
-    }
+        for (int j = 0; j < N; ++j) {
+            const float s2 = rate[lc + j];
+            float zs = 0.f, h = 0.f, p = 0.f;
+#pragma unroll
+            for (int t = 0; t < S; ++t) {
+                gr[t][j] = WHOLE || t0 + t < len ? sigmoid(gr[t][j]) : 0.f;
+                gi[t][j] = sigmoid(gi[t][j]);
+                const float z2 = s2 * gr[t][j];
+                d[t][j] = __builtin_amdgcn_exp2f(-z2);
+                u[t][j] *= __builtin_amdgcn_sqrtf(one_minus_square(d[t][j], z2)) * gi[t][j];
+                zs += z2;
+                h = __builtin_fmaf(d[t][j], h, u[t][j]);
+            }
+#pragma unroll
+            for (int t = S - 1; t >= 0; --t) p = d[t][j] * (gg[t][j] + p);
+            runs.a[seg][lc + j] = __builtin_amdgcn_exp2f(-zs);
+            runs.h[seg][lc + j] = h;
+            run_p[seg][lc + j] = p;
+        }
+    };
+    if (whole)
+        load(std::true_type{});
+    else
+        load(std::false_type{});
+    wave_order();
+    float A, H, Q;
+    join<R::PER, false>(runs.a, runs.h, wave * R::PER, lane, A, H);
+    runs.wave_a[wave][lane] = A;
+    runs.wave_h[wave][lane] = H;
+    join<R::PER, true>(runs.a, run_p, wave * R::PER, lane, A, Q);
+    wave_b[wave][lane] = A;
+    wave_p[wave][lane] = Q;
     __syncthreads();
-    if (tid < 64) {
+    if (wave == 0) {
         float handed = 0.f;
-        if (link == 0) {
-            if (a.d_last && c1 < a.D) handed = a.d_last[(int64_t)b * a.D + c1];
-        }
+        if (link == 0 && a.d_last && c1 < a.D) handed = a.d_last[(int64_t)b * a.D + c1];
         if (a.chunks > 1) {
-            const Chain c = chain_of(a.ws, columns, a.chunks, column);
-            float A = 1.f, Q = 0.f;
-#pragma unroll 8
-            for (int s = SEG - 1; s >= 0; --s) {
-                Q = __builtin_fmaf(run_a[s][tid], Q, run_p[s][tid]);
-                A *= run_a[s][tid];
-            }
+            const Chain c = chain_of(a.ws, columns, a.links, column);
+            join<WAVES, true>(wave_b, wave_p, 0, lane, A, Q);
             if (link > 0) {
-                publish(c, link, tid, A, Q);
-                handed = look_back(c, link, tid);
+                publish(c, link, lane, A, Q);
+                handed = look_back(c, link, lane);
             }
-            publish(c, link, tid, __builtin_fmaf(A, handed, Q));
+            publish(c, link, lane, __builtin_fmaf(A, handed, Q));
         }
-#pragma unroll 8
-        for (int s = SEG - 1; s >= 0; --s) {
-            const float next = __builtin_fmaf(run_a[s][tid], handed, run_p[s][tid]);
-            run_p[s][tid] = handed;
-            handed = next;
-        }
-    } else if (tid < 128) {
-        const int l = tid - 64;
-        float st = a.states[((int64_t)column * a.chunks + k) * kScanChannels + l];
-#pragma unroll 8
-        for (int s = 0; s < SEG; ++s) {
-            const float next = __builtin_fmaf(run_a[s][l], st, run_h[s][l]);
-            run_h[s][l] = st;
-            st = next;
-        }
+        enter<WAVES, true>(wave_b, wave_p, 0, lane, handed);
+    } else if (wave == 1) {
+        enter<WAVES, false>(runs.wave_a, runs.wave_h, 0, lane, a.states[((int64_t)column * a.chunks + k) * kScanChannels + lane]);
     }
     __syncthreads();
-    float esum[N];
+    enter<R::PER, false>(runs.a, runs.h, wave * R::PER, lane, runs.wave_h[wave][lane]);
+    enter<R::PER, true>(runs.a, run_p, wave * R::PER, lane, wave_p[wave][lane]);
+    wave_order();
+    float h[N], esum[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        h[j] = run_h[seg][lc + j];
-        p[j] = run_p[seg][lc + j];
+        h[j] = runs.h[seg][lc + j];
+        float p = run_p[seg][lc + j];
         esum[j] = 0.f;
 #pragma unroll
         for (int t = S - 1; t >= 0; --t) {
-            gg[t][j] += p[j];
-            p[j] = d[t][j] * gg[t][j];
+            gg[t][j] += p;
+            p = d[t][j] * gg[t][j];
         }
-    }
-    if (a.dh0 && k == 0 && seg == 0) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (j < n) a.dh0[(int64_t)b * a.D + ch + j] = p[j];
+        if (a.dh0 && k == 0 && seg == 0 && j < n) a.dh0[(int64_t)b * a.D + ch + j] = p;
     }
 #pragma unroll
     for (int t = 0; t < S; ++t) {
         float dx[N], dr[N], di[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const float z2 = s2[j] * gr[t][j], z = z2 * kLn2, m2 = one_minus_square(d[t][j], z2);
+            const float z2 = rate[lc + j] * gr[t][j], z = z2 * kLn2, m2 = one_minus_square(d[t][j], z2);
             const float v = gg[t][j] * u[t][j];
             // z / m^2 -> 1/2 as z -> 0, where u is 0 too
             const float over = z > 1e-30f ? z * __builtin_amdgcn_rcpf(m2) : 0.5f;
@@ -410,26 +482,34 @@ __global__ __launch_bounds__(512) void scan_bwd(ScanBwdArgs a) {
             dr[j] = e * (1.f - gr[t][j]);
             esum[j] += e;
         }
-        if (t0 + t < a.L) {
+        const int64_t at = ((int64_t)b * a.L + t0 + t) * a.D + ch;
+        if (whole) {
+            store_piece(static_cast<T*>(a.dx) + at, N, dx);
+            store_piece(static_cast<T*>(a.dr) + at, N, dr);
+            store_piece(static_cast<T*>(a.di) + at, N, di);
+        } else if (t0 + t < a.L) {
             if (t0 + t >= len) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) dx[j] = dr[j] = di[j] = 0.f;
             }
-            const int64_t at = ((int64_t)b * a.L + t0 + t) * a.D + ch;
             store_piece(static_cast<T*>(a.dx) + at, n, dx);
             store_piece(static_cast<T*>(a.dr) + at, n, dr);
             store_piece(static_cast<T*>(a.di) + at, n, di);
         }
     }
-    // the chunk's share of dlam, its runs added in order (run_a is taken)
+    // the chunk's share of dlam, its runs added in order (the wave's runs.a are taken)
 #pragma unroll
-    for (int j = 0; j < N; ++j) run_a[seg][lc + j] = esum[j];
+    for (int j = 0; j < N; ++j) runs.a[seg][lc + j] = esum[j];
+    wave_order();
+    float s = runs.a[wave * R::PER][lane];
+#pragma unroll
+    for (int q = 1; q < R::PER; ++q) s += runs.a[wave * R::PER + q][lane];
+    runs.wave_a[wave][lane] = s;
     __syncthreads();
-    if (tid < 64) {
-        float s = run_a[0][tid];
-#pragma unroll 8
-        for (int q = 1; q < SEG; ++q) s += run_a[q][tid];
-        a.shares[((int64_t)column * a.chunks + k) * kScanChannels + tid] = s;
+    if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s += runs.wave_a[w][lane];
+        a.shares[(((int64_t)b * a.chunks + k) * a.columns + g) * kScanChannels + lane] = s;
     }
 }
 
@@ -439,28 +519,10 @@ __global__ __launch_bounds__(256) void scan_bwd_empty(ScanBwdArgs a) {
     if (id < (int64_t)a.B * a.D) a.dh0[id] = a.d_last ? a.d_last[id] : 0.f;
 }
 
-// dlam: a workgroup takes a column, its 16 waves every 16th share each, added in wave order
 __global__ __launch_bounds__(1024) void scan_dlam(ScanBwdArgs a) {
-    __shared__ float part[16][kScanChannels];
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int c = (int)blockIdx.x * kScanChannels + lane;
-    const int64_t shares = (int64_t)a.B * a.chunks;
-    float t[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t s = wave; s < shares; s += 64)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int64_t q = s + 16 * v;
-            if (q < shares) {
-                const int64_t b = q / a.chunks, k = q - b * a.chunks;
-                t[v] += a.shares[((b * a.columns + blockIdx.x) * a.chunks + k) * kScanChannels + lane];
-            }
-        }
-    part[wave][lane] = (t[0] + t[1]) + (t[2] + t[3]);
-    __syncthreads();
-    if (wave == 0 && c < a.D) {
-        float s = part[0][lane];
-#pragma unroll
-        for (int w = 1; w < 16; ++w) s += part[w][lane];
+    const int64_t c0 = (int64_t)blockIdx.x * kSumColumns, c = c0 + threadIdx.x;
+    const float s = column_sum(a.shares, (int64_t)a.B * a.chunks, (int64_t)a.columns * kScanChannels, c0, a.D);
+    if (threadIdx.x < kSumColumns && c < a.D) {
         // d softplus / softplus; both are exp(lam) far below 0
         const float lam = a.lam[c];
         const float f = lam < -20.f ? 1.f : 1.f / ((1.f + expf(-lam)) * (fmaxf(lam, 0.f) + log1pf(expf(-fabsf(lam)))));
@@ -470,8 +532,19 @@ __global__ __launch_bounds__(1024) void scan_dlam(ScanBwdArgs a) {
 
 template <typename A>
 hipError_t clear_chain(const A& a, hipStream_t stream) {
-    const int64_t groups = scan_chain_bytes((int64_t)a.B * a.columns, a.chunks) / 4096 + 1;
+    const int64_t groups = scan_chain_bytes((int64_t)a.B * a.columns, a.links) / 4096 + 1;
     return launch<A>(&chain_clear<A>, groups < 1024 ? groups : 1024, 256, a, stream);
+}
+
+template <typename T, int CHUNK>
+hipError_t tiles(const ScanArgs& args, hipStream_t stream) {
+    ScanArgs a = args;
+    const int64_t columns = (int64_t)a.B * a.columns;
+    a.links = (int)(((int64_t)a.L + CHUNK - 1) / CHUNK);
+    if (a.links == 1) return launch<ScanArgs>(&scan_tiles<T, CHUNK, false>, columns, 2 * CHUNK, a, stream);
+    const hipError_t e = clear_chain(a, stream);
+    if (e != hipSuccess) return e;
+    return launch<ScanArgs>(&scan_tiles<T, CHUNK, true>, columns * a.links, 2 * CHUNK, a, stream);
 }
 
 template <typename T>
@@ -480,10 +553,7 @@ hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
     // a few tokens: a thread for each piece of channels, nothing to meet
     if (a.L <= 4)
         return launch<ScanArgs>(&scan_serial<T>, (columns * (kScanChannels / kVec<T>) + 255) / 256, 256, a, stream);
-    if (a.chunks == 1) return launch<ScanArgs>(&scan_tiles<T, false>, columns, 256, a, stream);
-    const hipError_t e = clear_chain(a, stream);
-    if (e != hipSuccess) return e;
-    return launch<ScanArgs>(&scan_tiles<T, true>, columns * a.chunks, 256, a, stream);
+    return columns * a.chunks >= 2 * a.cus ? tiles<T, 256>(a, stream) : tiles<T, 128>(a, stream);
 }
 template <typename T>
 hipError_t bwd(const ScanBwdArgs& a, hipStream_t stream) {
@@ -491,12 +561,12 @@ hipError_t bwd(const ScanBwdArgs& a, hipStream_t stream) {
     hipError_t e = hipSuccess;
     if (columns > 0 && a.chunks > 0) {
         if (a.chunks > 1) e = clear_chain(a, stream);
-        if (e == hipSuccess) e = launch<ScanBwdArgs>(&scan_bwd<T>, columns * a.chunks, 512, a, stream);
+        if (e == hipSuccess) e = launch<ScanBwdArgs>(&scan_bwd<T>, columns * a.chunks, kBwdThreads, a, stream);
     } else if (columns > 0 && a.dh0) {
         e = launch<ScanBwdArgs>(&scan_bwd_empty, ((int64_t)a.B * a.D + 255) / 256, 256, a, stream);
     }
     if (e != hipSuccess) return e;
-    return launch<ScanBwdArgs>(&scan_dlam, a.columns, 1024, a, stream);
+    return launch<ScanBwdArgs>(&scan_dlam, ((int64_t)a.D + kSumColumns - 1) / kSumColumns, 1024, a, stream);
 }
 
 }  // namespace

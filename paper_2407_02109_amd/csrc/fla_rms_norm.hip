@@ -370,25 +370,10 @@ __global__ __launch_bounds__(1024) void norm_bwd_wide(NormBwdArgs a) {
     }
 }
 
-// dweight: a workgroup takes 64 channels, its 16 waves every 16th share each, added in wave order
 __global__ __launch_bounds__(1024) void norm_bwd_weight(NormBwdArgs a) {
-    __shared__ float part[16][64];
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float t[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < a.D)
-        for (int b = wave; b < a.blocks; b += 64)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (b + 16 * u < a.blocks) t[u] += a.ws[(int64_t)(b + 16 * u) * a.D + c];
-    part[wave][lane] = (t[0] + t[1]) + (t[2] + t[3]);
-    __syncthreads();
-    if (wave == 0 && c < a.D) {
-        float s = part[0][lane];
-#pragma unroll
-        for (int w = 1; w < 16; ++w) s += part[w][lane];
-        a.dweight[c] = s;
-    }
+    const int64_t c0 = (int64_t)blockIdx.x * kSumColumns;
+    const float s = column_sum(a.ws, a.blocks, a.D, c0, a.D);
+    if (threadIdx.x < kSumColumns && c0 + threadIdx.x < a.D) a.dweight[c0 + threadIdx.x] = s;
 }
 
 // Waves per row and pieces per lane by the width: one wave up to 4 pieces a lane, then 4, then 16 (up to
@@ -442,7 +427,7 @@ hipError_t bwd(const NormBwdArgs& a, hipStream_t stream) {
         }
         if (e != hipSuccess) return e;
     }
-    return launch<NormBwdArgs>(&norm_bwd_weight, ((int64_t)a.D + 63) / 64, 1024, args, stream);
+    return launch<NormBwdArgs>(&norm_bwd_weight, ((int64_t)a.D + kSumColumns - 1) / kSumColumns, 1024, args, stream);
 }
 
 }  // namespace

@@ -441,6 +441,7 @@ int fla_gated_scan_fwd(const void* x, int64_t x_batch, int64_t x_token, const vo
     a.D = D;
     a.columns = (int)scan_columns(D);
     a.chunks = (int)scan_chunks(L);
+    a.cus = cus;
     a.c = c;
     return launched(fla::launch_scan_fwd(a, dtype == FLA_BF16, stream));
 }
@@ -505,7 +506,7 @@ int fla_gated_scan_bwd(const void* x, int64_t x_batch, int64_t x_token, const vo
     a.L = L;
     a.D = D;
     a.columns = (int)scan_columns(D);
-    a.chunks = (int)scan_chunks(L);
+    a.chunks = a.links = (int)scan_chunks(L);
     a.c = c;
     return launched(fla::launch_scan_bwd(a, dtype == FLA_BF16, stream));
 }

@@ -52,6 +52,35 @@ __device__ __forceinline__ void load_piece(const bf16_t* p, int n, float (&v)[8]
         for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.f;
     }
 }
+// a piece as it lies in memory: its first n values, the others 0
+__device__ __forceinline__ u32x4_any load_raw(const float* p, int n) {
+    u32x4_any w = {0u, 0u, 0u, 0u};
+    if (n >= 4) {
+        w = *reinterpret_cast<const u32x4_any*>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) w[j] = f32_bits(p[j]);
+    }
+    return w;
+}
+__device__ __forceinline__ u32x4_any load_raw(const bf16_t* p, int n) {
+    u32x4_any w = {0u, 0u, 0u, 0u};
+    if (n >= 8) {
+        w = *reinterpret_cast<const u32x4_any*>(p);
+    } else {
+        const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) w[j / 2] |= (unsigned)h[j] << 16 * (j % 2);
+    }
+    return w;
+}
+__device__ __forceinline__ void unpack(const u32x4_any& w, float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = bits_f32(w[j]);
+}
+__device__ __forceinline__ void unpack(const u32x4_any& w, float (&v)[8]) { unpack_piece(w, v); }
 // eight fp32 values beside a piece of eight bf16
 __device__ __forceinline__ void load_piece(const float* p, int n, float (&v)[8]) {
     float a[4], b[4];
@@ -122,6 +151,37 @@ __device__ __forceinline__ unsigned over_lanes(unsigned x, int lanes) {
     return x;
 }
 __device__ __forceinline__ float wave_sum(float x) { return bits_f32(over_lanes<SumOp>(f32_bits(x), 64)); }
+
+// ---- sums of columns: column c of [rows, stride] over the rows, for a workgroup of 1024 and kSumColumns columns from
+//      c0 on (those below `columns`); the result in the threads below kSumColumns.  Each thread adds every 64th row of
+//      a column, eight loads at a time; then the 64 sums in order.  Few columns a workgroup: a few hundred rows of some
+//      hundred columns are all there is, and only as many workgroups as that gives read them.
+constexpr int kSumColumns = 16;
+__device__ __forceinline__ float column_sum(const float* p, int64_t rows, int64_t stride, int64_t c0, int64_t columns) {
+    __shared__ float part[64][kSumColumns], quarter[16][kSumColumns];
+    const int col = (int)threadIdx.x % kSumColumns, slot = (int)threadIdx.x / kSumColumns;
+    float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c0 + col < columns) {
+        const float* q = p + c0 + col;
+        int64_t r = slot;
+        for (; r + 7 * 64 < rows; r += 8 * 64)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t[u] += q[(r + u * 64) * stride];
+#pragma unroll
+        for (int u = 0; u < 7; ++u)
+            if (r + u * 64 < rows) t[u] += q[(r + u * 64) * stride];
+    }
+    part[slot][col] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    __syncthreads();
+    if (slot < 16)
+        quarter[slot][col] = (part[4 * slot][col] + part[4 * slot + 1][col]) + (part[4 * slot + 2][col] + part[4 * slot + 3][col]);
+    __syncthreads();
+    float s = 0.f;
+    if (slot == 0)
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += quarter[w][col];
+    return s;
+}
 
 // ---- host side
 template <typename A>

@@ -71,7 +71,7 @@ constexpr int kRotaryTable = 512;   // (cos, sin) of one turn: tokens * rot / 2 
 hipError_t launch_rotary(const RotaryArgs& a, bool bf16, bool interleaved, int cus, hipStream_t stream);
 
 // ---- gated linear recurrence (fla_gated_scan.hip)
-constexpr int kScanChunk = 128;     // tokens
+constexpr int kScanChunk = 128;     // tokens from one kept state to the next
 constexpr int kScanChannels = 64;   // of a column
 struct ScanInput {
     const void* p;
@@ -88,6 +88,8 @@ struct ScanArgs {
     void* ws;                // the chain's words (several chunks)
     int B, L, D;
     int columns, chunks;
+    int links;               // of the chain: tiles of a column (set by the launcher)
+    int cus;
     float c;
 };
 struct ScanBwdArgs {
@@ -102,16 +104,17 @@ struct ScanBwdArgs {
     float* dlam;
     float* dh0;              // NULL: not wanted
     void* ws;                // the chain's words (several chunks)
-    float* shares;           // [B, columns, chunks, 64]: shares of dlam
+    float* shares;           // [B, chunks, columns, 64]: shares of dlam
     int B, L, D;
     int columns, chunks;
+    int links;               // == chunks
     float c;
 };
-// The chain's words: for each (column, chunk, channel) 12 bytes, then a ticket for each column, in cache lines of
-// their own.
+// The chain's words: 12 bytes for each (column, chunk, channel), a mark for each (column, chunk), and a ticket for each
+// column in cache lines of its own.
 constexpr int kScanTicketWords = 32;
 inline int64_t scan_chain_bytes(int64_t columns, int64_t chunks) {
-    return chunks > 1 ? columns * (chunks * kScanChannels * 12 + kScanTicketWords * 4) : 0;
+    return chunks > 1 ? columns * (chunks * (kScanChannels * 12 + 4) + kScanTicketWords * 4) : 0;
 }
 hipError_t launch_scan_fwd(const ScanArgs& a, bool bf16, hipStream_t stream);
 hipError_t launch_scan_bwd(const ScanBwdArgs& a, bool bf16, hipStream_t stream);

@@ -10,6 +10,8 @@ inline float __builtin_amdgcn_rcpf(float x) { return 1.f / x; }
 inline float __builtin_amdgcn_rsqf(float x) { return 1.f / std::sqrt(x); }
 inline float __builtin_amdgcn_sqrtf(float x) { return std::sqrt(x); }
 inline void __builtin_amdgcn_s_sleep(int) {}
+inline void __builtin_amdgcn_wave_barrier() { emu_wave_barrier(); }
+inline void __builtin_amdgcn_fence(int, const char*) {}
 inline void sincospif(float x, float* s, float* c) {
     const double t = 3.14159265358979323846 * (double)x;
     *s = (float)std::sin(t);
