@@ -83,7 +83,7 @@ int fla_add_rms_norm_bwd(const void* dy, int64_t dy_stride, const void* s, int64
  * the others with axis 1 (rot divisible by 4).  Any value is a position, negative ones too.
  * freqs [rot / 2]: float64, radians per unit of position.  Angles are formed in 64 bits, so far
  * positions keep their place in the turn; cosine and sine are rounded to fp32 once.
- * Strides per tensor: batch, token, head.  q_out may be exactly q (same strides), k_out exactly k:
+ * Strides per tensor: batch, token, head (the last below 2^32: FLA_ERR_TOO_LARGE).  q_out may be exactly q (same strides), k_out exactly k:
  * in place.  Tokens may not overlap in an output. */
 int fla_rotary(const void* q, int64_t q_batch, int64_t q_token, int64_t q_head,
                const void* k, int64_t k_batch, int64_t k_token, int64_t k_head,

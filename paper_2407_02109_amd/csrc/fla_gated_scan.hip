@@ -39,6 +39,13 @@ struct Tile {
     static constexpr int S = CHUNK / SEG;            // tokens of a run
     static constexpr int WAVES = THREADS / 64;
 };
+// Forward: up to kSerial tokens a thread runs over them for two channels (us a call, bf16, serial against tiles of 128:
+// 64 x 16 tokens x 2048 channels 18.5, 24.3; 64 x 32 33.7, 23.1; 1 x 16 x 768 10.7, 9.4; 1 x 1 x 768 3.2, 7.8).  More
+// tokens: tiles of kFwdChunk, or of half of it where that holds all of them (16 x 128 x 1024 7.6, in tiles of 256
+// 11.3).  Tiles of 128 in a chain have twice the links to wait for: 1 x 65536 x 256 72.7 instead of 50.1,
+// 1 x 30450 x 768 70.6 instead of 61.0, 8 x 1024 x 2048 37.5 and 39.0.
+constexpr int kFwdChunk = 256;
+constexpr int kSerial = 16;
 constexpr int kBwdThreads = 512;
 
 __device__ __forceinline__ float sigmoid(float v) {
@@ -73,10 +80,10 @@ __device__ __forceinline__ const T* row_of(const ScanInput& m, int b, int64_t t)
     return static_cast<const T*>(m.p) + (b * m.batch + t * m.token);
 }
 
-// One thread for each piece of channels of a sequence, token by token.
+// A thread for two channels of a sequence, token by token.
 template <typename T>
 __global__ __launch_bounds__(256) void scan_serial(ScanArgs a) {
-    constexpr int N = kVec<T>, X = kScanChannels / N;
+    constexpr int N = 2, X = kScanChannels / N;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int per_b = a.columns * X;
     if (id >= (int64_t)a.B * per_b) return;
@@ -352,8 +359,8 @@ __global__ __launch_bounds__(2 * CHUNK, 4) void scan_tiles(ScanArgs a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) h[j] = __builtin_fmaf(d[t][j], h[j], u[t][j]);
         T* row = static_cast<T*>(a.h) + ((int64_t)b * a.L + t0 + t) * a.D + ch;
-        if (whole)
-            store_piece(row, N, h);
+        if (whole && a.lines)
+            store_piece<true>(row, N, h);
         else
             store_piece(row, n, h);
         if (a.h_last && t0 + t == len - 1) {
@@ -483,10 +490,10 @@ __global__ __launch_bounds__(kBwdThreads, 4) void scan_bwd(ScanBwdArgs a) {
             esum[j] += e;
         }
         const int64_t at = ((int64_t)b * a.L + t0 + t) * a.D + ch;
-        if (whole) {
-            store_piece(static_cast<T*>(a.dx) + at, N, dx);
-            store_piece(static_cast<T*>(a.dr) + at, N, dr);
-            store_piece(static_cast<T*>(a.di) + at, N, di);
+        if (whole && a.lines) {
+            store_piece<true>(static_cast<T*>(a.dx) + at, N, dx);
+            store_piece<true>(static_cast<T*>(a.dr) + at, N, dr);
+            store_piece<true>(static_cast<T*>(a.di) + at, N, di);
         } else if (t0 + t < a.L) {
             if (t0 + t >= len) {
 #pragma unroll
@@ -536,24 +543,18 @@ hipError_t clear_chain(const A& a, hipStream_t stream) {
     return launch<A>(&chain_clear<A>, groups < 1024 ? groups : 1024, 256, a, stream);
 }
 
-template <typename T, int CHUNK>
-hipError_t tiles(const ScanArgs& args, hipStream_t stream) {
+template <typename T>
+hipError_t fwd(const ScanArgs& args, hipStream_t stream) {
     ScanArgs a = args;
     const int64_t columns = (int64_t)a.B * a.columns;
-    a.links = (int)(((int64_t)a.L + CHUNK - 1) / CHUNK);
-    if (a.links == 1) return launch<ScanArgs>(&scan_tiles<T, CHUNK, false>, columns, 2 * CHUNK, a, stream);
+    if (a.L <= kSerial) return launch<ScanArgs>(&scan_serial<T>, (columns * (kScanChannels / 2) + 255) / 256, 256, a, stream);
+    a.links = (int)(((int64_t)a.L + kFwdChunk - 1) / kFwdChunk);
+    if (a.L <= kFwdChunk / 2)
+        return launch<ScanArgs>(&scan_tiles<T, kFwdChunk / 2, false>, columns, kFwdChunk, a, stream);
+    if (a.links == 1) return launch<ScanArgs>(&scan_tiles<T, kFwdChunk, false>, columns, 2 * kFwdChunk, a, stream);
     const hipError_t e = clear_chain(a, stream);
     if (e != hipSuccess) return e;
-    return launch<ScanArgs>(&scan_tiles<T, CHUNK, true>, columns * a.links, 2 * CHUNK, a, stream);
-}
-
-template <typename T>
-hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
-    const int64_t columns = (int64_t)a.B * a.columns;
-    // a few tokens: a thread for each piece of channels, nothing to meet
-    if (a.L <= 4)
-        return launch<ScanArgs>(&scan_serial<T>, (columns * (kScanChannels / kVec<T>) + 255) / 256, 256, a, stream);
-    return columns * a.chunks >= 2 * a.cus ? tiles<T, 256>(a, stream) : tiles<T, 128>(a, stream);
+    return launch<ScanArgs>(&scan_tiles<T, kFwdChunk, true>, columns * a.links, 2 * kFwdChunk, a, stream);
 }
 template <typename T>
 hipError_t bwd(const ScanBwdArgs& a, hipStream_t stream) {

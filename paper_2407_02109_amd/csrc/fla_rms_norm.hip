@@ -72,7 +72,11 @@ __device__ __forceinline__ void store_q(unsigned char* p, int n, const float (&y
         w[j] = (unsigned)u;
     }
     if (n >= N) {
-        __builtin_memcpy(p, w, N);
+        // non-temporal: 121800 rows of 1024 bf16 take 138 us instead of 162 (with the sum so stored too 148)
+        if constexpr (N == 8)
+            store8<true>(p, u32x2_any{w[0], w[1]});
+        else
+            __builtin_memcpy(p, w, N);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
@@ -99,14 +103,14 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_fwd(NormArgs a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = (k * 64 * W + rw.first) * N;
-            load_piece(x + col, a.D - col, s[k]);
+            load_piece<true>(x + col, a.D - col, s[k]);
         }
         if (res) {
             float t[K][N];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int col = (k * 64 * W + rw.first) * N;
-                load_piece(res + col, a.D - col, t[k]);
+                load_piece<true>(res + col, a.D - col, t[k]);
             }
 #pragma unroll
             for (int k = 0; k < K; ++k)

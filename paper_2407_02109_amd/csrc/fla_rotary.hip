@@ -9,16 +9,28 @@
 #include "fla_seq_device.h"
 #include "fla_seq_internal.h"
 
+#include <type_traits>
+
 namespace fla {
 namespace {
 
-template <typename T, bool PAIRS>
+constexpr int kRows = 2;     // heads that a thread has in flight
+constexpr int kTokens = 64;  // of one turn, at most
+
+// WHOLE: every piece of a head is a whole one.
+template <typename T, bool PAIRS, bool WHOLE>
 __global__ __launch_bounds__(256) void rotary(RotaryArgs a) {
     constexpr int N = kVec<T>;
     __shared__ float2 table[kRotaryTable + N];   // a last piece reads past its pairs, and drops that
+    __shared__ T* place[2][2][kTokens];          // of each token's first head: q and k, in and out
     const int half = a.rot >> 1;
     const int slots = 256 / a.pieces;            // heads that the workgroup turns at a time
     const int slot = (int)threadIdx.x / a.pieces, piece = (int)threadIdx.x - slot * a.pieces;
+    const bool turns_here = piece < a.turn_pieces;
+    const int c = turns_here ? piece * N : a.rot + (piece - a.turn_pieces) * N;
+    const int n = WHOLE ? N : !turns_here ? a.d - c : PAIRS ? a.rot - c : half - c;
+    // channels that are copied have nothing to do in place
+    const bool idle_q = !turns_here && a.q.in == a.q.out, idle_k = !turns_here && a.k.in == a.k.out;
     const int64_t turns = (a.n_tokens + a.tokens - 1) / a.tokens;
     for (int64_t g = blockIdx.x; g < turns; g += gridDim.x) {
         const unsigned tok0 = (unsigned)(g * a.tokens);
@@ -31,58 +43,73 @@ __global__ __launch_bounds__(256) void rotary(RotaryArgs a) {
                                        : (double)static_cast<const int*>(a.positions)[at];
             double rev = pos * a.freqs[j] * 0.15915494309189533577;   // 1 / (2 pi)
             rev -= __builtin_rint(rev);
-            float s, c;
-            sincospif(2.f * (float)rev, &s, &c);
-            table[e] = make_float2(c * a.mscale, s * a.mscale * a.sign);
+            float s, co;
+            sincospif(2.f * (float)rev, &s, &co);
+            table[e] = make_float2(co * a.mscale, s * a.mscale * a.sign);
+        }
+        if ((int)threadIdx.x < nt) {
+            const unsigned b = a.div_L.div(tok0 + threadIdx.x), l = tok0 + threadIdx.x - b * (unsigned)a.L;
+            auto first = [&](const void* p, int64_t batch, int64_t token) {
+                return const_cast<T*>(static_cast<const T*>(p)) + (b * batch + l * token);
+            };
+            place[0][0][threadIdx.x] = first(a.q.in, a.q.in_batch, a.q.in_token);
+            place[0][1][threadIdx.x] = first(a.q.out, a.q.out_batch, a.q.out_token);
+            place[1][0][threadIdx.x] = first(a.k.in, a.k.in_batch, a.k.in_token);
+            place[1][1][threadIdx.x] = first(a.k.out, a.k.out_batch, a.k.out_token);
         }
         __syncthreads();
-        if (slot < slots)
-            for (int row = slot; row < nt * a.heads; row += slots) {
+        const int rows = slot < slots ? nt * a.heads : 0;
+        // kRows heads at a time: their loads before the first store, which may be in place of them
+        for (int row0 = slot; row0 < rows; row0 += kRows * slots) {
+            u32x4_any v[kRows], w[kRows];
+            T* out[kRows];
+            int pair[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                out[u] = nullptr;
+                const int row = row0 + u * slots;
+                if (row >= rows) continue;
                 const int t = (int)a.div_heads.div((unsigned)row);
-                int h = row - t * a.heads;
-                const unsigned b = a.div_L.div(tok0 + t), l = tok0 + t - b * (unsigned)a.L;
-                const bool is_q = h < a.hq;
-                if (!is_q) h -= a.hq;
-                const RotaryTensor& m = is_q ? a.q : a.k;
-                const T* in = static_cast<const T*>(m.in) + (b * m.in_batch + l * m.in_token + h * m.in_head);
-                T* out = static_cast<T*>(m.out) + (b * m.out_batch + l * m.out_token + h * m.out_head);
-                if (piece >= a.turn_pieces) {
-                    const int c = a.rot + (piece - a.turn_pieces) * N;
-                    float v[N];
-                    if (m.in != m.out) {
-                        load_piece(in + c, a.d - c, v);
-                        store_piece(out + c, a.d - c, v);
-                    }
+                const int head = row - t * a.heads;
+                const bool is_q = head < a.hq;
+                if (is_q ? idle_q : idle_k) continue;
+                const unsigned h = (unsigned)(is_q ? head : head - a.hq);
+                const T* in = place[is_q ? 0 : 1][0][t] + (uint64_t)h * (is_q ? a.q.in_head : a.k.in_head) + c;
+                out[u] = place[is_q ? 0 : 1][1][t] + (uint64_t)h * (is_q ? a.q.out_head : a.k.out_head) + c;
+                pair[u] = t * half + (PAIRS ? c >> 1 : c);
+                v[u] = load_raw<true>(in, n);
+                if (!PAIRS && turns_here) w[u] = load_raw<true>(in + half, n);
+            }
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                if (!out[u]) continue;
+                float x[N], y[N];
+                unpack(v[u], x);
+                if (!turns_here) {
+                    store_piece(out[u], n, x);
                 } else if constexpr (PAIRS) {
-                    const int c = piece * N, n = a.rot - c;
-                    const float2* cs = table + t * half + (c >> 1);
-                    float v[N];
-                    load_piece(in + c, n, v);
 #pragma unroll
                     for (int j = 0; j < N / 2; ++j) {
-                        const float2 w = cs[j];
-                        const float x = v[2 * j], y = v[2 * j + 1];
-                        v[2 * j] = x * w.x - y * w.y;
-                        v[2 * j + 1] = y * w.x + x * w.y;
+                        const float2 cs = table[pair[u] + j];
+                        const float a0 = x[2 * j], b0 = x[2 * j + 1];
+                        x[2 * j] = a0 * cs.x - b0 * cs.y;
+                        x[2 * j + 1] = b0 * cs.x + a0 * cs.y;
                     }
-                    store_piece(out + c, n, v);
+                    store_piece(out[u], n, x);
                 } else {
-                    const int c = piece * N, n = half - c;
-                    const float2* cs = table + t * half + c;
-                    float x[N], y[N];
-                    load_piece(in + c, n, x);
-                    load_piece(in + half + c, n, y);
+                    unpack(w[u], y);
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
-                        const float2 w = cs[j];
-                        const float u = x[j] * w.x - y[j] * w.y;
-                        y[j] = y[j] * w.x + x[j] * w.y;
-                        x[j] = u;
+                        const float2 cs = table[pair[u] + j];
+                        const float t0 = x[j] * cs.x - y[j] * cs.y;
+                        y[j] = y[j] * cs.x + x[j] * cs.y;
+                        x[j] = t0;
                     }
-                    store_piece(out + c, n, x);
-                    store_piece(out + half + c, n, y);
+                    store_piece(out[u], n, x);
+                    store_piece(out[u] + half, n, y);
                 }
             }
+        }
         __syncthreads();   // the next turn writes the table
     }
 }
@@ -94,16 +121,22 @@ hipError_t launch_rotary(const RotaryArgs& args, bool bf16, bool interleaved, in
     const int vec = bf16 ? 8 : 4, half = a.rot / 2;
     a.turn_pieces = interleaved ? (a.rot + vec - 1) / vec : (half + vec - 1) / vec;
     a.pieces = a.turn_pieces + (a.d - a.rot + vec - 1) / vec;
-    // a table entry for each thread, but four workgroups for each compute unit before several tokens in one
-    const int64_t spread = (a.n_tokens + 4 * cus - 1) / (4 * cus);
-    const int fit = half < 256 ? 256 / half : 1;
+    // a table entry for each thread, but eight workgroups for each compute unit before several tokens in one
+    const int64_t spread = (a.n_tokens + 8 * cus - 1) / (8 * cus);
+    const int fit = half >= 256 ? 1 : half > 256 / kTokens ? 256 / half : kTokens;
     a.tokens = (int)(spread < fit ? spread : fit);
     a.div_L = FastDiv::make((unsigned)a.L);
     a.div_half = FastDiv::make((unsigned)half);
     a.div_heads = FastDiv::make((unsigned)a.heads);
     const int64_t turns = (a.n_tokens + a.tokens - 1) / a.tokens, most = (int64_t)cus * 64;
-    auto* kernel = bf16 ? (interleaved ? &rotary<bf16_t, true> : &rotary<bf16_t, false>)
-                        : (interleaved ? &rotary<float, true> : &rotary<float, false>);
+    const bool whole = (interleaved ? a.rot : half) % vec == 0 && (a.d - a.rot) % vec == 0;
+    auto pick = [&](auto t, auto pairs) {
+        using T = decltype(t);
+        constexpr bool P = decltype(pairs)::value;
+        return whole ? &rotary<T, P, true> : &rotary<T, P, false>;
+    };
+    auto* kernel = bf16 ? (interleaved ? pick(bf16_t{}, std::true_type{}) : pick(bf16_t{}, std::false_type{}))
+                        : (interleaved ? pick(float{}, std::true_type{}) : pick(float{}, std::false_type{}));
     return launch<RotaryArgs>(kernel, turns < most ? turns : most, 256, a, stream);
 }
 

@@ -183,6 +183,11 @@ int64_t scan_ws_bytes(int B, int L, int D) { return fla::scan_chain_bytes(B * sc
 // the chain's words and the chunks' shares of dlam
 int64_t scan_bwd_ws_bytes(int B, int L, int D) { return scan_ws_bytes(B, L, D) + scan_states_bytes(B, L, D); }
 
+// whether rows of D elements from p on begin at cache lines
+bool lines(const void* p, int D, int elem) {
+    return (int64_t)D * elem % 128 == 0 && reinterpret_cast<uintptr_t>(p) % 128 == 0;
+}
+
 int scan_bytes(int B, int L, int D, size_t* bytes, int64_t (*of)(int, int, int)) {
     const int st = scan_sizes(B, L, D);
     if (st != FLA_OK) return st;
@@ -328,6 +333,7 @@ int fla_rotary(const void* q, int64_t q_batch, int64_t q_token, int64_t q_head, 
         in[i] = {m.heads ? m.in : nullptr, m.s[0], m.s[1], B, L, wi, e};
         out[i] = {m.heads ? m.out : nullptr, m.s[6], m.s[7], B, L, wo, e};
         if (in[i].elements() >= kMaxElems || out[i].elements() >= kMaxElems) return FLA_ERR_TOO_LARGE;
+        if (m.heads > 1 && (m.s[2] > UINT32_MAX || m.s[8] > UINT32_MAX)) return FLA_ERR_TOO_LARGE;
     }
     const Range pos = {positions, (reach(B, pos_batch) + reach(L, pos_token) + axes) * (pos64 ? 8 : 4)};
     const Range table = {freqs, (int64_t)rot / 2 * 8};
@@ -364,8 +370,8 @@ int fla_rotary(const void* q, int64_t q_batch, int64_t q_token, int64_t q_head, 
     const int st = check_arch(&cus);
     if (st != FLA_OK) return st;
     fla::RotaryArgs a{};
-    a.q = {q, q_out, q_batch, q_token, q_head, qo_batch, qo_token, qo_head};
-    a.k = {k, k_out, k_batch, k_token, k_head, ko_batch, ko_token, ko_head};
+    a.q = {q, q_out, q_batch, q_token, qo_batch, qo_token, (unsigned)q_head, (unsigned)qo_head};
+    a.k = {k, k_out, k_batch, k_token, ko_batch, ko_token, (unsigned)k_head, (unsigned)ko_head};
     a.positions = positions;
     a.freqs = freqs;
     a.pos_batch = pos_batch;
@@ -442,6 +448,7 @@ int fla_gated_scan_fwd(const void* x, int64_t x_batch, int64_t x_token, const vo
     a.columns = (int)scan_columns(D);
     a.chunks = (int)scan_chunks(L);
     a.cus = cus;
+    a.lines = lines(h, D, e);
     a.c = c;
     return launched(fla::launch_scan_fwd(a, dtype == FLA_BF16, stream));
 }
@@ -507,6 +514,7 @@ int fla_gated_scan_bwd(const void* x, int64_t x_batch, int64_t x_token, const vo
     a.D = D;
     a.columns = (int)scan_columns(D);
     a.chunks = a.links = (int)scan_chunks(L);
+    a.lines = lines(dx, D, e) && lines(dr, D, e) && lines(di, D, e);
     a.c = c;
     return launched(fla::launch_scan_bwd(a, dtype == FLA_BF16, stream));
 }

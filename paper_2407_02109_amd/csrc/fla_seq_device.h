@@ -12,7 +12,33 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 // 16, 8 and 4 bytes at any element's address (global memory takes them at any alignment)
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// 16 or 8 bytes, of values that are not used again soon (NT: the non-temporal cache policy) or as usual.  (The
+// types are named here: as a template's argument they would lose their alignment.)
+template <bool NT>
+__device__ __forceinline__ u32x4_any load16(const void* p) {
+    const u32x4_any* q = static_cast<const u32x4_any*>(p);
+    if constexpr (NT)
+        return __builtin_nontemporal_load(q);
+    else
+        return *q;
+}
+template <bool NT>
+__device__ __forceinline__ void store16(void* p, const u32x4_any& v) {
+    u32x4_any* q = static_cast<u32x4_any*>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(v, q);
+    else
+        *q = v;
+}
+template <bool NT>
+__device__ __forceinline__ void store8(void* p, const u32x2_any& v) {
+    u32x2_any* q = static_cast<u32x2_any*>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(v, q);
+    else
+        *q = v;
+}
 
 // values of a type in 16 bytes
 template <typename T>
@@ -27,11 +53,12 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b) {
 }
 
 // the first n values of a 16-byte piece at p (the others 0); n >= kVec: the whole piece
+template <bool NT = false>
 __device__ __forceinline__ void load_piece(const float* p, int n, float (&v)[4]) {
     if (n >= 4) {
-        const f32x4_any w = *reinterpret_cast<const f32x4_any*>(p);
+        const u32x4_any w = load16<NT>(p);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = w[j];
+        for (int j = 0; j < 4; ++j) v[j] = bits_f32(w[j]);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = j < n ? p[j] : 0.f;
@@ -44,19 +71,21 @@ __device__ __forceinline__ void unpack_piece(const u32x4_any& w, float (&v)[8]) 
         v[2 * j + 1] = bits_f32(w[j] & 0xffff0000u);
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void load_piece(const bf16_t* p, int n, float (&v)[8]) {
     if (n >= 8) {
-        unpack_piece(*reinterpret_cast<const u32x4_any*>(p), v);
+        unpack_piece(load16<NT>(p), v);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = j < n ? (float)p[j] : 0.f;
     }
 }
 // a piece as it lies in memory: its first n values, the others 0
+template <bool NT = false>
 __device__ __forceinline__ u32x4_any load_raw(const float* p, int n) {
     u32x4_any w = {0u, 0u, 0u, 0u};
     if (n >= 4) {
-        w = *reinterpret_cast<const u32x4_any*>(p);
+        w = load16<NT>(p);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -64,10 +93,11 @@ __device__ __forceinline__ u32x4_any load_raw(const float* p, int n) {
     }
     return w;
 }
+template <bool NT = false>
 __device__ __forceinline__ u32x4_any load_raw(const bf16_t* p, int n) {
     u32x4_any w = {0u, 0u, 0u, 0u};
     if (n >= 8) {
-        w = *reinterpret_cast<const u32x4_any*>(p);
+        w = load16<NT>(p);
     } else {
         const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
@@ -92,29 +122,44 @@ __device__ __forceinline__ void load_piece(const float* p, int n, float (&v)[8])
         v[4 + j] = b[j];
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void store_piece(float* p, int n, const float (&v)[4]) {
     if (n >= 4) {
-        f32x4_any w;
+        u32x4_any w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[j];
-        *reinterpret_cast<f32x4_any*>(p) = w;
+        for (int j = 0; j < 4; ++j) w[j] = f32_bits(v[j]);
+        store16<NT>(p, w);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (j < n) p[j] = v[j];
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void store_piece(bf16_t* p, int n, const float (&v)[8]) {
     if (n >= 8) {
         u32x4_any w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-        *reinterpret_cast<u32x4_any*>(p) = w;
+        store16<NT>(p, w);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) p[j] = (bf16_t)v[j];
     }
+}
+
+// two values
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* p, int n, float (&v)[2]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) v[j] = j < n ? (float)p[j] : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, int n, const float (&v)[2]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        if (j < n) p[j] = (T)v[j];
 }
 
 // ---- over the lanes of a wave.  Lane permutations inside 16 lanes are operands of the vector ALU:

@@ -50,7 +50,8 @@ hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream);
 struct RotaryTensor {
     const void* in;
     void* out;               // == in: in place
-    int64_t in_batch, in_token, in_head, out_batch, out_token, out_head;
+    int64_t in_batch, in_token, out_batch, out_token;
+    unsigned in_head, out_head;
 };
 struct RotaryArgs {
     RotaryTensor q, k;
@@ -90,6 +91,7 @@ struct ScanArgs {
     int columns, chunks;
     int links;               // of the chain: tiles of a column (set by the launcher)
     int cus;
+    int lines;               // the columns' rows of h are whole cache lines
     float c;
 };
 struct ScanBwdArgs {
@@ -108,6 +110,7 @@ struct ScanBwdArgs {
     int B, L, D;
     int columns, chunks;
     int links;               // == chunks
+    int lines;               // the columns' rows of dx, dr and di are whole cache lines
     float c;
 };
 // The chain's words: 12 bytes for each (column, chunk, channel), a mark for each (column, chunk), and a ticket for each

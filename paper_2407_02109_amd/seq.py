@@ -152,40 +152,54 @@ def fla_gated_scan_bwd(x, x_strides, r, r_strides, i, i_strides, lam, states, le
 
 # ---- tensors -------------------------------------------------------------------------------------
 
+_codes = {}
+
+
 def _dtype(t):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return FLA_BF16
-    if t.dtype == torch.float32:
-        return FLA_F32
-    raise TypeError("tensors must be bfloat16 or float32, got %s" % t.dtype)
+    code = _codes.get(t.dtype)
+    if code is None:
+        import torch
+        _codes.update({torch.float32: FLA_F32, torch.bfloat16: FLA_BF16})
+        code = _codes.get(t.dtype)
+        if code is None:
+            raise TypeError("tensors must be bfloat16 or float32, got %s" % t.dtype)
+    return code
 
 
 def _on(t, stream, body):
     """body(raw stream) with t's device current, on `stream` or that device's current one."""
     import torch
-    if not t.is_cuda:
+    device = t.device
+    if device.type != "cuda":
         raise ValueError("tensors must be on the GPU")
     if stream is None:
-        if t.device.index == torch.cuda.current_device():
-            return body(torch.cuda.current_stream().cuda_stream)
-        with torch.cuda.device(t.device):
-            return body(torch.cuda.current_stream().cuda_stream)
+        if device.index == torch.cuda.current_device():
+            return body(torch._C._cuda_getCurrentRawStream(device.index))
+        with torch.cuda.device(device):
+            return body(torch._C._cuda_getCurrentRawStream(device.index))
     if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream, t.device) if stream else torch.cuda.default_stream(t.device)
-    if stream.device != t.device:
-        raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, t.device))
+        stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    if stream.device != device:
+        raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, device))
     with torch.cuda.stream(stream):
         return body(stream.cuda_stream)
 
 
+def _new(like):
+    """A contiguous tensor of like's shape and type."""
+    import torch
+    return torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
 def _same(name, t, like, shape, dtype=None):
     """t on like's device, of this shape and type (default: like's)."""
-    if t.dtype != (like.dtype if dtype is None else dtype):
-        raise TypeError("%s must be %s, got %s" % (name, like.dtype if dtype is None else dtype, t.dtype))
+    if dtype is None:
+        dtype = like.dtype
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.device != like.device:
         raise ValueError("%s is on %s, expected %s" % (name, t.device, like.device))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:   # (a torch.Size compares as a tuple)
         raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
 
 
@@ -200,7 +214,7 @@ def _rows(name, t):
     """Elements between the rows of a [..., D] tensor with contiguous channels and evenly spaced rows."""
     if t.dim() == 0:
         raise ValueError("%s must have channels" % name)
-    if t.numel() == 0 or t.is_contiguous():
+    if t.is_contiguous() or t.numel() == 0:
         return t.shape[-1]
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("%s must have contiguous channels" % name)
@@ -219,9 +233,10 @@ def _rows(name, t):
 
 def _strides(name, t):
     """All strides but the last, of a tensor with contiguous channels."""
-    if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
+    *strides, last = t.stride()
+    if last != 1 and t.shape[-1] > 1 and t.numel():
         raise ValueError("%s must have contiguous channels" % name)
-    return t.stride()[:-1]
+    return strides
 
 
 def _norm_args(x, weight, residual):
@@ -248,10 +263,10 @@ def _norm_fwd(x, weight, residual, eps, out, sum_out, keep, stream):
             _whole(name, t, x, x.shape)
 
     def body(raw):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        y = _new(x) if out is None else out
         s = sum_out
         if s is None and residual is not None:
-            s = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            s = _new(x)
         rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if keep else None
         fla_add_rms_norm_fwd(x, stride, residual, rstride, weight, y, s, rstd, rows, D, eps, dtype, wdtype, raw)
         return y, x if s is None else s, rstd
@@ -289,7 +304,7 @@ def add_rms_norm_q8(x, weight, residual=None, eps=1e-6, group=0, sum_out=None, s
         scales = torch.empty((*x.shape[:-1], -(-D // group) if group else 1), dtype=torch.float32, device=x.device)
         s = sum_out
         if s is None and residual is not None:
-            s = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            s = _new(x)
         fla_add_rms_norm_q8(x, stride, residual, rstride, weight, q, scales, s, rows, D, group, eps, dtype, wdtype, raw)
         return q, scales, x if s is None else s
 
@@ -308,7 +323,7 @@ def add_rms_norm_bwd(dy, s, weight, rstd, dsum=None, stream=None):
         dsstride = _rows("dsum", dsum)
 
     def body(raw):
-        dx = torch.empty(s.shape, dtype=s.dtype, device=s.device)
+        dx = _new(s)
         dw = torch.empty(D, dtype=torch.float32, device=s.device)
         nbytes = fla_add_rms_norm_bwd_workspace(rows, D)
         ws = torch.empty(nbytes, dtype=torch.uint8, device=s.device)
@@ -369,10 +384,10 @@ def _rotary(q, k, freqs, positions, interleaved, mscale, out, inverse, stream):
         _same("out[1]", ko, k, k.shape)
 
     def body(raw):
-        qr = torch.empty(q.shape, dtype=q.dtype, device=q.device) if qo is None else qo
+        qr = _new(q) if qo is None else qo
         kr = ko
         if kr is None and k is not None:
-            kr = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            kr = _new(k)
         fla_rotary(q, qstr, k, kstr, qr, _strides("out[0]", qr), kr, _strides("out[1]", kr) if hk else (0, 0, 0),
                    positions, int(positions.dtype == torch.int64), positions.stride(0), positions.stride(1), axes,
                    freqs, B, L, hq, hk, d, 2 * freqs.shape[0], int(interleaved), mscale, inverse, dtype, raw)
@@ -419,7 +434,7 @@ def _scan_fwd(x, r, i, lam, h0, lengths, c, out, keep, stream):
         _whole("out", out, x, x.shape)
 
     def body(raw):
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        h = _new(x) if out is None else out
         last = torch.empty((B, D), dtype=torch.float32, device=x.device)
         states = torch.empty(fla_gated_scan_states(B, L, D) // 4, dtype=torch.float32, device=x.device) if keep else None
         nbytes = fla_gated_scan_workspace(B, L, D)
@@ -459,8 +474,8 @@ def gated_scan_step(x, r, i, lam, state, c=8.0, out=None, new_state=None, stream
         _whole("out", out, x, (B, D))
 
     def body(raw):
-        h = torch.empty((B, D), dtype=x.dtype, device=x.device) if out is None else out
-        ns = torch.empty((B, D), dtype=torch.float32, device=x.device) if new_state is None else new_state
+        h = _new(x) if out is None else out
+        ns = _new(state) if new_state is None else new_state
         fla_gated_scan_fwd(x, (xs[0], 0), r, (rs[0], 0), i, (is_[0], 0), lam, state, None, h, ns, None, None, 0, B, 1,
                            D, c, dtype, raw)
         return h, ns
@@ -483,7 +498,7 @@ def gated_scan_bwd(x, r, i, lam, states, dh, d_last=None, lengths=None, c=8.0, s
         _whole("d_last", d_last, x, (B, D), torch.float32)
 
     def body(raw):
-        dx, dr, di = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(3))
+        dx, dr, di = _new(x), _new(x), _new(x)
         dlam = torch.empty(D, dtype=torch.float32, device=x.device)
         dh0 = torch.empty((B, D), dtype=torch.float32, device=x.device)
         nbytes = fla_gated_scan_bwd_workspace(B, L, D)

@@ -6,6 +6,10 @@
 
 extern thread_local emu_index gridDim;
 
+// (the host's own want aligned addresses)
+#define __builtin_nontemporal_load(p) (*(p))
+#define __builtin_nontemporal_store(v, p) (*(p) = (v))
+
 inline float __builtin_amdgcn_rcpf(float x) { return 1.f / x; }
 inline float __builtin_amdgcn_rsqf(float x) { return 1.f / std::sqrt(x); }
 inline float __builtin_amdgcn_sqrtf(float x) { return std::sqrt(x); }

@@ -227,7 +227,7 @@ def _scan_inputs(B, L, D, dt, seed, lam_mean=-3.0):
 
 
 # B, L, D, lengths
-SCAN_SHAPES = [(1, 1, 1, None), (64, 1, 200, None), (3, 2, 9, None), (2, 31, 70, None), (2, 128, 64, None), (1, 129, 65, None),
+SCAN_SHAPES = [(1, 1, 1, None), (64, 1, 200, None), (3, 2, 9, None), (2, 16, 66, [16, 3]), (2, 17, 64, None), (1, 256, 70, None), (2, 31, 70, None), (2, 128, 64, None), (1, 129, 65, None),
                (2, 257, 130, [0, 257]), (4, 300, 66, [1, 128, 129, 300]), (1, 1000, 33, None), (2, 4100, 24, [4100, 2049]),
                (3, 640, 1001, [640, 1, 333]), (1, 9000, 8, None)]
 
