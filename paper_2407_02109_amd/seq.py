@@ -67,6 +67,11 @@ def _done(rc, check=True):
     return rc
 
 
+def _at(t):
+    """A tensor's address, or None."""
+    return None if t is None else t.data_ptr()
+
+
 def _size(fn, *args) -> int:
     n = ctypes.c_size_t()
     _check(fn(*args, ctypes.byref(n)))
@@ -268,7 +273,9 @@ def _norm_fwd(x, weight, residual, eps, out, sum_out, keep, stream):
         if s is None and residual is not None:
             s = _new(x)
         rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if keep else None
-        fla_add_rms_norm_fwd(x, stride, residual, rstride, weight, y, s, rstd, rows, D, eps, dtype, wdtype, raw)
+        _done(load_seq_library().fla_add_rms_norm_fwd(
+            x.data_ptr(), stride, _at(residual), rstride, weight.data_ptr(), y.data_ptr(), _at(s), _at(rstd), rows, D, eps,
+            dtype, wdtype, raw))
         return y, x if s is None else s, rstd
 
     return _on(x, stream, body)
@@ -388,9 +395,11 @@ def _rotary(q, k, freqs, positions, interleaved, mscale, out, inverse, stream):
         kr = ko
         if kr is None and k is not None:
             kr = _new(k)
-        fla_rotary(q, qstr, k, kstr, qr, _strides("out[0]", qr), kr, _strides("out[1]", kr) if hk else (0, 0, 0),
-                   positions, int(positions.dtype == torch.int64), positions.stride(0), positions.stride(1), axes,
-                   freqs, B, L, hq, hk, d, 2 * freqs.shape[0], int(interleaved), mscale, inverse, dtype, raw)
+        _done(load_seq_library().fla_rotary(
+            q.data_ptr(), *qstr, _at(k), *kstr, qr.data_ptr(), *_strides("out[0]", qr), _at(kr),
+            *(_strides("out[1]", kr) if hk else kstr), positions.data_ptr(), positions.dtype == torch.int64,
+            *positions.stride()[:2], axes, freqs.data_ptr(), B, L, hq, hk, d, 2 * freqs.shape[0], interleaved, mscale,
+            inverse, dtype, raw))
         return qr, kr
 
     return _on(q, stream, body)
@@ -476,8 +485,9 @@ def gated_scan_step(x, r, i, lam, state, c=8.0, out=None, new_state=None, stream
     def body(raw):
         h = _new(x) if out is None else out
         ns = _new(state) if new_state is None else new_state
-        fla_gated_scan_fwd(x, (xs[0], 0), r, (rs[0], 0), i, (is_[0], 0), lam, state, None, h, ns, None, None, 0, B, 1,
-                           D, c, dtype, raw)
+        _done(load_seq_library().fla_gated_scan_fwd(
+            x.data_ptr(), xs[0], 0, r.data_ptr(), rs[0], 0, i.data_ptr(), is_[0], 0, lam.data_ptr(), state.data_ptr(), None,
+            h.data_ptr(), ns.data_ptr(), None, None, 0, B, 1, D, c, dtype, raw))
         return h, ns
 
     return _on(x, stream, body)
