@@ -250,7 +250,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide(NormArgs a) {
 
 // ---- backward: a workgroup takes every gridDim-th row (of W = 1: four at a time) and keeps its share of
 //      dweight in registers, which goes to the workspace at the end and is summed by norm_bwd_weight.
-template <typename T, int W, int K>
+// (NT: rows of whole cache lines, read non-temporally)
+template <typename T, int W, int K, bool NT>
 __global__ __launch_bounds__(Row<W>::kThreads) void norm_bwd(NormBwdArgs a) {
     constexpr int N = kVec<T>;
     __shared__ unsigned red[2][16];
@@ -272,8 +273,8 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_bwd(NormBwdArgs a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = (k * 64 * W + rw.first) * N;
-            load_piece(sp + col, a.D - col, s[k]);
-            load_piece(dyp + col, a.D - col, dy[k]);
+            load_piece<NT>(sp + col, a.D - col, s[k]);
+            load_piece<NT>(dyp + col, a.D - col, dy[k]);
         }
         float along = 0.f;
 #pragma unroll
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_bwd(NormBwdArgs a) {
             const int col = (k * 64 * W + rw.first) * N;
             float t[N];
             if (ds) {
-                load_piece(ds + col, a.D - col, t);
+                load_piece<NT>(ds + col, a.D - col, t);
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j) t[j] = 0.f;
@@ -380,28 +381,47 @@ __global__ __launch_bounds__(1024) void norm_bwd_weight(NormBwdArgs a) {
     if (threadIdx.x < kSumColumns && c0 + threadIdx.x < a.D) a.dweight[c0 + threadIdx.x] = s;
 }
 
-// Waves per row and pieces per lane by the width: one wave up to 4 pieces a lane, then 4, then 16 (up to
-// MOST pieces).
-template <int MOST, typename F>
-bool by_width(int D, int vec, F&& f) {
-    const int64_t pieces = ((int64_t)D + vec - 1) / vec;
+// Waves per row and pieces per lane by the width.
 #define FLA_WIDTH(W, K) \
     if (pieces <= 64 * W * K) { f(std::integral_constant<int, W>{}, std::integral_constant<int, K>{}); return true; }
+// Forward: one wave up to 4 pieces a lane, then 4, then 16.
+template <typename F>
+bool fwd_width(int64_t pieces, F&& f) {
     FLA_WIDTH(1, 1)
     FLA_WIDTH(1, 2)
     FLA_WIDTH(1, 4)
     FLA_WIDTH(4, 2)
     FLA_WIDTH(4, 4)
     FLA_WIDTH(16, 2)
-    if constexpr (MOST == 4) FLA_WIDTH(16, 4)
-#undef FLA_WIDTH
+    FLA_WIDTH(16, 4)
     return false;
 }
+// Backward, where a lane keeps four values for each channel: as few pieces of bf16 as the waves allow (with 4 in a
+// lane two waves fit a SIMD: 8192 rows of 2048 43 us, with one and four waves a row 35), up to 4 of fp32.
+template <typename T, typename F>
+bool bwd_width(int64_t pieces, F&& f) {
+    FLA_WIDTH(1, 1)
+    FLA_WIDTH(1, 2)
+    if constexpr (sizeof(T) == 4) {
+        FLA_WIDTH(1, 4)
+        FLA_WIDTH(4, 2)
+        FLA_WIDTH(4, 4)
+        FLA_WIDTH(16, 2)
+        FLA_WIDTH(16, 4)
+    } else {
+        FLA_WIDTH(4, 1)
+        FLA_WIDTH(4, 2)
+        FLA_WIDTH(16, 1)
+        FLA_WIDTH(16, 2)
+    }
+    return false;
+}
+#undef FLA_WIDTH
 
 template <typename T, bool Q8>
 hipError_t fwd(const NormArgs& a, int cus, hipStream_t stream) {
     hipError_t e = hipErrorInvalidValue;
-    const bool kept = by_width<4>(a.D, kVec<T>, [&](auto w, auto k) {
+    const bool kept = fwd_width(((int64_t)a.D + kVec<T> - 1) / kVec<T>, [&](auto w, auto k) {
         constexpr int W = decltype(w)::value, K = decltype(k)::value;
         const int64_t need = (a.rows + Row<W>::kRows - 1) / Row<W>::kRows;
         const int64_t most = (int64_t)cus * (W == 16 ? 4 : 16);
@@ -418,15 +438,16 @@ hipError_t bwd(const NormBwdArgs& a, hipStream_t stream) {
     NormBwdArgs args = a;
     args.blocks = 0;
     if (a.rows > 0) {
-        auto blocks = [&](int64_t need) { return (int)(need < kNormBwdBlocks ? need : kNormBwdBlocks); };
-        // (16 waves of 4 pieces of bf16 do not fit their 128 registers)
-        const bool kept = by_width<sizeof(T) == 2 ? 2 : 4>(a.D, kVec<T>, [&](auto w, auto k) {
+        const int most = norm_bwd_blocks(a.rows, a.D);
+        const bool kept = bwd_width<T>(((int64_t)a.D + kVec<T> - 1) / kVec<T>, [&](auto w, auto k) {
             constexpr int W = decltype(w)::value, K = decltype(k)::value;
-            args.blocks = blocks((a.rows + Row<W>::kRows - 1) / Row<W>::kRows);
-            e = launch<NormBwdArgs>(&norm_bwd<T, W, K>, args.blocks, Row<W>::kThreads, args, stream);
+            const int64_t need = (a.rows + Row<W>::kRows - 1) / Row<W>::kRows;
+            args.blocks = (int)(need < most ? need : most);
+            e = launch<NormBwdArgs>(a.lines ? &norm_bwd<T, W, K, true> : &norm_bwd<T, W, K, false>, args.blocks,
+                                    Row<W>::kThreads, args, stream);
         });
         if (!kept) {
-            args.blocks = blocks(a.rows);
+            args.blocks = most;
             e = launch<NormBwdArgs>(&norm_bwd_wide<T>, args.blocks, 1024, args, stream);
         }
         if (e != hipSuccess) return e;

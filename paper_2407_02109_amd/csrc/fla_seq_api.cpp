@@ -92,6 +92,11 @@ bool share(const Tokens& a, const Tokens& b) {
     return d < a.wide * a.elem || d + b.wide * b.elem > period;
 }
 
+// whether rows of `stride` elements from p on begin at cache lines
+bool lines(const void* p, int64_t stride, int elem) {
+    return stride * elem % 128 == 0 && reinterpret_cast<uintptr_t>(p) % 128 == 0;
+}
+
 // ---- norm
 
 int norm_checks(int64_t rows, int D, const int64_t* strides, int n_strides, float eps, int dtype, int weight_dtype) {
@@ -183,11 +188,6 @@ int64_t scan_ws_bytes(int B, int L, int D) { return fla::scan_chain_bytes(B * sc
 // the chain's words and the chunks' shares of dlam
 int64_t scan_bwd_ws_bytes(int B, int L, int D) { return scan_ws_bytes(B, L, D) + scan_states_bytes(B, L, D); }
 
-// whether rows of D elements from p on begin at cache lines
-bool lines(const void* p, int D, int elem) {
-    return (int64_t)D * elem % 128 == 0 && reinterpret_cast<uintptr_t>(p) % 128 == 0;
-}
-
 int scan_bytes(int B, int L, int D, size_t* bytes, int64_t (*of)(int, int, int)) {
     const int st = scan_sizes(B, L, D);
     if (st != FLA_OK) return st;
@@ -219,8 +219,7 @@ int fla_add_rms_norm_bwd_workspace(int64_t rows, int D, size_t* bytes) {
     if (rows < 0 || D < 0) return FLA_ERR_SHAPE;
     if (!bytes) return FLA_ERR_NULL;
     if (D > kMaxWidth) return FLA_ERR_TOO_LARGE;
-    const int64_t blocks = rows < fla::kNormBwdBlocks ? rows : fla::kNormBwdBlocks;
-    *bytes = (size_t)(blocks * D * 4);
+    *bytes = (size_t)fla::norm_bwd_blocks(rows, D) * D * 4;
     return FLA_OK;
 }
 
@@ -275,6 +274,7 @@ int fla_add_rms_norm_bwd(const void* dy, int64_t dy_stride, const void* s, int64
     a.D = D;
     a.weight_f32 = weight_dtype == FLA_F32;
     a.inv_D = (float)(1.0 / D);
+    a.lines = lines(dy, dy_stride, e) && lines(s, s_stride, e) && (!dsum || lines(dsum, dsum_stride, e));
     return launched(fla::launch_norm_bwd(a, dtype == FLA_BF16, stream));
 }
 

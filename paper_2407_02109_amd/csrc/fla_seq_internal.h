@@ -42,8 +42,15 @@ struct NormBwdArgs {
     int weight_f32;
     float inv_D;
     int blocks;
+    int lines;               // rows are whole cache lines
 };
-constexpr int kNormBwdBlocks = 512;   // at most: two for each compute unit of the chip
+// Workgroups of the backward at most, each with a share of dweight in the workspace: about as many as the chip holds
+// of them (rows of up to 512 channels: a few registers, of more than 4096: 16 waves).  us a call, bf16, for 512 / 1024 /
+// 256: 65536 rows of 768 144, 91, 246; 131072 of 256 147, 88, 261; 4096 of 16384 128, 156, 117.
+inline int norm_bwd_blocks(int64_t rows, int D) {
+    const int most = D <= 512 ? 1536 : D <= 4096 ? 1024 : 256;
+    return rows < most ? (int)rows : most;
+}
 hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream);
 
 // ---- rotary positions (fla_rotary.hip)

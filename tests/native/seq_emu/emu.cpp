@@ -6,9 +6,34 @@
 #include <vector>
 
 #include <sanitizer/common_interface_defs.h>
-#include <ucontext.h>
 
 #include "fla_seq_internal.h"
+
+// saves the callee-saved registers and the stack pointer at *from, and goes on where `to` was saved (x86-64)
+extern "C" void emu_switch(void** from, void* to);
+asm(R"(
+    .text
+    .globl emu_switch
+    .hidden emu_switch
+    .type emu_switch, @function
+emu_switch:
+    pushq %rbp
+    pushq %rbx
+    pushq %r12
+    pushq %r13
+    pushq %r14
+    pushq %r15
+    movq %rsp, (%rdi)
+    movq %rsi, %rsp
+    popq %r15
+    popq %r14
+    popq %r13
+    popq %r12
+    popq %rbx
+    popq %rbp
+    ret
+    .size emu_switch, .-emu_switch
+)");
 
 thread_local emu_index threadIdx, blockIdx, gridDim;
 
@@ -17,14 +42,14 @@ constexpr unsigned kEmuMaxWaves = 16;
 constexpr size_t kStack = 256 << 10;
 enum State { kRuns, kAtWave, kAtBlock, kEnded };
 struct Item {
-    ucontext_t ctx;
+    void* sp;
     std::unique_ptr<unsigned char[]> stack;
     State state;
     unsigned exchanges;   // of this lane so far: every lane of a wave counts the same
     void* fake_stack;
 };
 std::vector<Item> g_items(64 * kEmuMaxWaves);
-ucontext_t g_main;
+void* g_main;
 const void* g_main_stack;
 size_t g_main_size;
 unsigned g_now;
@@ -37,7 +62,7 @@ void leave(State s) {
     Item& it = g_items[g_now];
     it.state = s;
     __sanitizer_start_switch_fiber(s == kEnded ? nullptr : &it.fake_stack, g_main_stack, g_main_size);
-    swapcontext(&it.ctx, &g_main);
+    emu_switch(&it.sp, g_main);
     __sanitizer_finish_switch_fiber(it.fake_stack, &g_main_stack, &g_main_size);
 }
 }  // namespace
@@ -87,11 +112,11 @@ static void run_block(unsigned n) {
     for (unsigned t = 0; t < n; ++t) {
         Item& it = g_items[t];
         if (!it.stack) it.stack.reset(new unsigned char[kStack]);
-        getcontext(&it.ctx);
-        it.ctx.uc_stack.ss_sp = it.stack.get();
-        it.ctx.uc_stack.ss_size = kStack;
-        it.ctx.uc_link = nullptr;
-        makecontext(&it.ctx, item_main, 0);
+        // six registers, then where the first switch returns to, with the stack as a call leaves it
+        void** top = reinterpret_cast<void**>((reinterpret_cast<uintptr_t>(it.stack.get()) + kStack) & ~uintptr_t(15)) - 1;
+        *--top = reinterpret_cast<void*>(&item_main);
+        for (int r = 0; r < 6; ++r) *--top = nullptr;
+        it.sp = top;
         it.state = kRuns;
         it.exchanges = 0;
         it.fake_stack = nullptr;
@@ -104,7 +129,7 @@ static void run_block(unsigned n) {
             threadIdx = {t, 0, 0};
             void* fake = nullptr;
             __sanitizer_start_switch_fiber(&fake, it.stack.get(), kStack);
-            swapcontext(&g_main, &it.ctx);
+            emu_switch(&g_main, it.sp);
             __sanitizer_finish_switch_fiber(fake, nullptr, nullptr);
             ended += it.state == kEnded;
         }

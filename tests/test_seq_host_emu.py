@@ -53,7 +53,8 @@ def library(tmp_path_factory):
 @pytest.mark.parametrize("group", ["norm", "norm_wide", "rotary", "scan"])
 def test_kernels_on_the_host(library, group):
     lib, runtime = library
-    env = dict(os.environ, LD_PRELOAD=runtime, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1:verify_asan_link_order=0")
+    env = dict(os.environ, LD_PRELOAD=runtime, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1:verify_asan_link_order=0:"
+                                                                    "detect_stack_use_after_return=0")
     r = subprocess.run([sys.executable, os.path.join(SEQ_EMU, "drive.py"), lib, group], capture_output=True, text=True,
                        timeout=900, env=env)
     assert r.returncode == 0 and r.stdout.rstrip().endswith("ok"), r.stdout[-1500:] + r.stderr[-4000:]
