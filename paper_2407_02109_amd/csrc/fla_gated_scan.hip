@@ -212,6 +212,16 @@ __device__ __forceinline__ float look_back(const Chain& c, int link, int lane) {
     return __builtin_nanf("");
 }
 
+// The column of a workgroup.  Ids go to the 8 XCDs in turn: in long chains groups of 8 take a column each, so that the
+// tiles of one chunk mostly meet in one XCD's L2 -- where the columns' rows are not whole cache lines and share some,
+// or HBM pages.  us a call, each id the next column / groups of 8: 1 x 20000 x 1001 bf16 79.5, 65.7; 4 x 5001 x 1001
+// 74.8, 64.2; 1 x 65536 x 768 102, 99.  Of few links the start of the chain counts: 4 x 2048 x 512 15.0, 15.9; and a
+// last group that is not full draws for nothing: 8 x 1024 x 2048 38.4, 44.3.
+__host__ __device__ constexpr int column_shift(int links, int lines) { return links >= (lines ? 32 : 16) ? 3 : 0; }
+__device__ __forceinline__ unsigned column_of(unsigned id, unsigned columns, int links, int lines) {
+    return (id >> column_shift(links, lines)) % columns;
+}
+
 // the words of a workspace before a chain: all ones; the marks and tickets 0
 template <typename A>
 __global__ __launch_bounds__(256) void chain_clear(A a) {
@@ -275,7 +285,7 @@ __global__ __launch_bounds__(2 * CHUNK, 4) void scan_tiles(ScanArgs a) {
     __shared__ float rate[kScanChannels];
     __shared__ int drawn;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = tid / X, lc = tid % X * N;
-    const unsigned columns = (unsigned)(a.B * a.columns), column = blockIdx.x % columns;
+    const unsigned columns = (unsigned)(a.B * a.columns), column = CHAIN ? column_of(blockIdx.x, columns, a.links, a.lines) : blockIdx.x;
     const int g = (int)(column % (unsigned)a.columns), b = (int)(column / (unsigned)a.columns);
     const int ch = g * kScanChannels + lc, n = a.D - ch;
     const int c1 = g * kScanChannels + lane;   // the channel of a joining lane
@@ -283,6 +293,7 @@ __global__ __launch_bounds__(2 * CHUNK, 4) void scan_tiles(ScanArgs a) {
     if (tid < 64) rate[tid] = c1 < a.D ? decay_rate(a.lam[c1], a.c) : 0.f;
     __syncthreads();
     const int k = CHAIN ? drawn : 0;
+    if (k >= a.links) return;
     const int len = length_of(a.lengths, b, a.L);
     const int t0 = k * CHUNK + seg * S;
     float d[S][N], u[S][N];
@@ -384,7 +395,7 @@ __global__ __launch_bounds__(kBwdThreads, 4) void scan_bwd(ScanBwdArgs a) {
     __shared__ float rate[kScanChannels];
     __shared__ int drawn;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, seg = tid / X, lc = tid % X * N;
-    const unsigned columns = (unsigned)(a.B * a.columns), column = blockIdx.x % columns;
+    const unsigned columns = (unsigned)(a.B * a.columns), column = column_of(blockIdx.x, columns, a.links, a.lines);
     const int g = (int)(column % (unsigned)a.columns), b = (int)(column / (unsigned)a.columns);
     const int ch = g * kScanChannels + lc, n = a.D - ch;
     const int c1 = g * kScanChannels + lane;   // the channel of a joining lane
@@ -392,6 +403,7 @@ __global__ __launch_bounds__(kBwdThreads, 4) void scan_bwd(ScanBwdArgs a) {
     if (tid < 64) rate[tid] = c1 < a.D ? decay_rate(a.lam[c1], a.c) : 0.f;
     __syncthreads();
     const int link = drawn, k = a.chunks - 1 - link;
+    if (link >= a.links) return;
     const int len = length_of(a.lengths, b, a.L);
     const int t0 = k * kScanChunk + seg * S;
     float d[S][N], u[S][N], gi[S][N], gr[S][N], gg[S][N];
@@ -543,6 +555,13 @@ hipError_t clear_chain(const A& a, hipStream_t stream) {
     return launch<A>(&chain_clear<A>, groups < 1024 ? groups : 1024, 256, a, stream);
 }
 
+// one workgroup for each tile, whole groups for each column (a workgroup that draws past the last link ends)
+template <typename A>
+int64_t chain_groups(const A& a) {
+    const int group = 1 << column_shift(a.links, a.lines);
+    return (int64_t)a.B * a.columns * ((a.links + group - 1) / group * group);
+}
+
 template <typename T>
 hipError_t fwd(const ScanArgs& args, hipStream_t stream) {
     ScanArgs a = args;
@@ -554,7 +573,7 @@ hipError_t fwd(const ScanArgs& args, hipStream_t stream) {
     if (a.links == 1) return launch<ScanArgs>(&scan_tiles<T, kFwdChunk, false>, columns, 2 * kFwdChunk, a, stream);
     const hipError_t e = clear_chain(a, stream);
     if (e != hipSuccess) return e;
-    return launch<ScanArgs>(&scan_tiles<T, kFwdChunk, true>, columns * a.links, 2 * kFwdChunk, a, stream);
+    return launch<ScanArgs>(&scan_tiles<T, kFwdChunk, true>, chain_groups(a), 2 * kFwdChunk, a, stream);
 }
 template <typename T>
 hipError_t bwd(const ScanBwdArgs& a, hipStream_t stream) {
@@ -562,7 +581,7 @@ hipError_t bwd(const ScanBwdArgs& a, hipStream_t stream) {
     hipError_t e = hipSuccess;
     if (columns > 0 && a.chunks > 0) {
         if (a.chunks > 1) e = clear_chain(a, stream);
-        if (e == hipSuccess) e = launch<ScanBwdArgs>(&scan_bwd<T>, columns * a.chunks, kBwdThreads, a, stream);
+        if (e == hipSuccess) e = launch<ScanBwdArgs>(&scan_bwd<T>, chain_groups(a), kBwdThreads, a, stream);
     } else if (columns > 0 && a.dh0) {
         e = launch<ScanBwdArgs>(&scan_bwd_empty, ((int64_t)a.B * a.D + 255) / 256, 256, a, stream);
     }
