@@ -81,8 +81,9 @@ int fla_add_rms_norm_bwd(const void* dy, int64_t dy_stride, const void* s, int64
  * positions: int32 or (pos64 != 0) int64, [B, L] or, with axes = 2, [B, L, 2] (axis contiguous), with
  * the strides pos_batch and pos_token: pairs of the first half (j < rot / 4) then turn with axis 0,
  * the others with axis 1 (rot divisible by 4).  Any value is a position, negative ones too.
- * freqs [rot / 2]: float64, radians per unit of position.  Angles are formed in 64 bits, so far
- * positions keep their place in the turn; cosine and sine are rounded to fp32 once.
+ * freqs [rot / 2]: float64, radians per unit of position.  Angles are formed in 64 bits (off by about 2^-52 of
+ * their size), so far positions keep their place in the turn; cosine and sine are rounded to fp32 once.
+ * B * L up to 2^31 - 1024, hq + hk up to 2^20, tensors below 2^40 elements (FLA_ERR_TOO_LARGE).
  * Strides per tensor: batch, token, head (the last below 2^32: FLA_ERR_TOO_LARGE).  q_out may be exactly q (same strides), k_out exactly k:
  * in place.  Tokens may not overlap in an output. */
 int fla_rotary(const void* q, int64_t q_batch, int64_t q_token, int64_t q_head,
@@ -120,7 +121,9 @@ int fla_rotary_freqs(int rot, double theta, int scaling, double factor, double t
  * Outputs: h [B, L, D] contiguous, h_last [B, D] fp32: the state behind each sequence's last token
  * (h0 for an empty one; NULL: not kept; it may be exactly h0), states: for the backward (NULL: not
  * kept), fla_gated_scan_states() bytes, contents private to the pair.
- * c finite and > 0 (FLA_ERR_UNSUPPORTED).  L = 1 is a step of a kept state.
+ * c finite and > 0 (FLA_ERR_UNSUPPORTED).  D up to 2^24, fewer than 2^22 tiles of 128 tokens by 64 channels, tensors
+ * below 2^40 elements (FLA_ERR_TOO_LARGE).  L = 1 is a step of a kept state.  A sequence's h does not depend on
+ * the others of its batch.
  * L = 0 with B, D > 0 copies h0 (or zeros) to h_last.
  * workspace: fla_gated_scan_workspace() bytes (may be NULL where that is 0); contents ignored on
  * entry.  Calls that may run at the same time need workspaces of their own. */

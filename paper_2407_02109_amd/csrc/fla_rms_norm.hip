@@ -63,7 +63,7 @@ __device__ __forceinline__ float scale_of(unsigned top_bits) {
 }
 // N values times 1 / scale as e4m3 bytes.  |y| / scale is at most 448 (1 + 2^-22), which rounds to 448.
 template <int N>
-__device__ __forceinline__ void store_q(unsigned char* p, int n, const float (&y)[N], float inv) {
+__device__ __forceinline__ void store_q(bool nt, unsigned char* p, int n, const float (&y)[N], float inv) {
     unsigned w[N / 4];
 #pragma unroll
     for (int j = 0; j < N / 4; ++j) {
@@ -72,11 +72,15 @@ __device__ __forceinline__ void store_q(unsigned char* p, int n, const float (&y
         w[j] = (unsigned)u;
     }
     if (n >= N) {
-        // non-temporal: 121800 rows of 1024 bf16 take 138 us instead of 162 (with the sum so stored too 148)
-        if constexpr (N == 8)
-            store8<true>(p, u32x2_any{w[0], w[1]});
-        else
+        if constexpr (N == 8) {
+            const u32x2_any v = {w[0], w[1]};
+            if (nt)
+                store8<true>(p, v);
+            else
+                store8<false>(p, v);
+        } else {
             __builtin_memcpy(p, w, N);
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_fwd(NormArgs a) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int col = (k * 64 * W + rw.first) * N;
-                store_piece(out + col, a.D - col, s[k]);
+                store_piece(a.nt, out + col, a.D - col, s[k]);
             }
         }
         const float rstd = __builtin_amdgcn_rsqf(
@@ -142,7 +146,7 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_fwd(NormArgs a) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int col = (k * 64 * W + rw.first) * N;
-                store_piece(y + col, a.D - col, s[k]);
+                store_piece(a.nt, y + col, a.D - col, s[k]);
             }
         } else {
             unsigned top[K];
@@ -167,7 +171,7 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_fwd(NormArgs a) {
                 const float scale = scale_of(a.group ? top[k] : top[0]);
                 if (col < a.D && (a.group ? (piece & (lanes - 1)) == 0 : piece == 0))
                     a.scales[row * groups + (a.group ? col / a.group : 0)] = scale;
-                store_q(q + col, a.D - col, s[k], 1.f / scale);
+                store_q(a.nt, q + col, a.D - col, s[k], 1.f / scale);
             }
         }
     }
@@ -242,7 +246,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide(NormArgs a) {
                 const float scale = scale_of(top);
                 if (a.group && col < a.D && (rw.first & (lanes - 1)) == 0)
                     a.scales[row * groups + col / a.group] = scale;
-                store_q(static_cast<unsigned char*>(a.y) + row * a.D + col, a.D - col, y, 1.f / scale);
+                store_q(false, static_cast<unsigned char*>(a.y) + row * a.D + col, a.D - col, y, 1.f / scale);
             }
         }
     }
@@ -419,7 +423,10 @@ bool bwd_width(int64_t pieces, F&& f) {
 #undef FLA_WIDTH
 
 template <typename T, bool Q8>
-hipError_t fwd(const NormArgs& a, int cus, hipStream_t stream) {
+hipError_t fwd(const NormArgs& args, int cus, hipStream_t stream) {
+    NormArgs a = args;
+    const int64_t per_row = (int64_t)a.D * (sizeof(T) * (1 + (a.residual != nullptr) + (a.sum != nullptr)) + (Q8 ? 1 : sizeof(T)));
+    a.nt = a.rows > kLastLevelCache / per_row;
     hipError_t e = hipErrorInvalidValue;
     const bool kept = fwd_width(((int64_t)a.D + kVec<T> - 1) / kVec<T>, [&](auto w, auto k) {
         constexpr int W = decltype(w)::value, K = decltype(k)::value;

@@ -17,8 +17,8 @@ namespace {
 constexpr int kRows = 2;     // heads that a thread has in flight
 constexpr int kTokens = 64;  // of one turn, at most
 
-// WHOLE: every piece of a head is a whole one.
-template <typename T, bool PAIRS, bool WHOLE>
+// WHOLE: every piece of a head is a whole one.  NT: outputs are stored non-temporally.
+template <typename T, bool PAIRS, bool WHOLE, bool NT>
 __global__ __launch_bounds__(256) void rotary(RotaryArgs a) {
     constexpr int N = kVec<T>;
     __shared__ float2 table[kRotaryTable + N];   // a last piece reads past its pairs, and drops that
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256) void rotary(RotaryArgs a) {
                 float x[N], y[N];
                 unpack(v[u], x);
                 if (!turns_here) {
-                    store_piece(out[u], n, x);
+                    store_piece<NT>(out[u], n, x);
                 } else if constexpr (PAIRS) {
 #pragma unroll
                     for (int j = 0; j < N / 2; ++j) {
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void rotary(RotaryArgs a) {
                         x[2 * j] = a0 * cs.x - b0 * cs.y;
                         x[2 * j + 1] = b0 * cs.x + a0 * cs.y;
                     }
-                    store_piece(out[u], n, x);
+                    store_piece<NT>(out[u], n, x);
                 } else {
                     unpack(w[u], y);
 #pragma unroll
@@ -105,8 +105,8 @@ __global__ __launch_bounds__(256) void rotary(RotaryArgs a) {
                         y[j] = y[j] * cs.x + x[j] * cs.y;
                         x[j] = t0;
                     }
-                    store_piece(out[u], n, x);
-                    store_piece(out[u] + half, n, y);
+                    store_piece<NT>(out[u], n, x);
+                    store_piece<NT>(out[u] + half, n, y);
                 }
             }
         }
@@ -130,10 +130,11 @@ hipError_t launch_rotary(const RotaryArgs& args, bool bf16, bool interleaved, in
     a.div_heads = FastDiv::make((unsigned)a.heads);
     const int64_t turns = (a.n_tokens + a.tokens - 1) / a.tokens, most = (int64_t)cus * 64;
     const bool whole = (interleaved ? a.rot : half) % vec == 0 && (a.d - a.rot) % vec == 0;
+    const bool large = 2 * a.n_tokens * a.heads * a.d * (bf16 ? 2 : 4) > kLastLevelCache;
     auto pick = [&](auto t, auto pairs) {
         using T = decltype(t);
         constexpr bool P = decltype(pairs)::value;
-        return whole ? &rotary<T, P, true> : &rotary<T, P, false>;
+        return !whole ? &rotary<T, P, false, false> : large ? &rotary<T, P, true, true> : &rotary<T, P, true, false>;
     };
     auto* kernel = bf16 ? (interleaved ? pick(bf16_t{}, std::true_type{}) : pick(bf16_t{}, std::false_type{}))
                         : (interleaved ? pick(float{}, std::true_type{}) : pick(float{}, std::false_type{}));

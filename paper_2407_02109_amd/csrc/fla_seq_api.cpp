@@ -13,7 +13,7 @@ namespace {
 constexpr int64_t kMaxElems = int64_t(1) << 40;
 constexpr int64_t kMaxGroups = (int64_t(1) << 22) - 1;   // grid.x * 1024 threads < 2^32
 constexpr int64_t kMaxLen = (int64_t(1) << 31) - 1024;   // tokens of a sequence
-constexpr int kMaxWidth = 1 << 24;                       // channels of a norm's row
+constexpr int kMaxWidth = 1 << 24;                       // channels of a norm's row or of a scan
 
 // Per-device probe result: 0 = not probed yet, -1 = not gfx950, > 0 = gfx950 with that many compute units.
 std::atomic<int> g_cus[64];
@@ -176,7 +176,7 @@ int scan_sizes(int B, int L, int D) { return B < 0 || L < 0 || D < 0 ? FLA_ERR_S
 int64_t scan_columns(int D) { return ((int64_t)D + fla::kScanChannels - 1) / fla::kScanChannels; }
 int64_t scan_chunks(int L) { return ((int64_t)L + fla::kScanChunk - 1) / fla::kScanChunk; }
 bool scan_too_large(int B, int L, int D) {
-    if (L > kMaxLen) return true;
+    if (L > kMaxLen || D > kMaxWidth) return true;
     const int64_t columns = scan_columns(D), chunks = scan_chunks(L);
     if ((int64_t)B * columns > kMaxGroups) return true;
     return chunks > 0 && (int64_t)B * columns > kMaxGroups / chunks;

@@ -162,6 +162,19 @@ __device__ __forceinline__ void store_piece(T* p, int n, const float (&v)[2]) {
         if (j < n) p[j] = (T)v[j];
 }
 
+// a piece, non-temporally if nt (which is the same for the whole launch)
+template <typename T, int N>
+__device__ __forceinline__ void store_piece(bool nt, T* p, int n, const float (&v)[N]) {
+    if (nt)
+        store_piece<true>(p, n, v);
+    else
+        store_piece<false>(p, n, v);
+}
+// Whether outputs are stored non-temporally: where the call's bytes pass the last-level cache, so that what it writes would
+// not be found there anyway.  us a call, as usual / non-temporally: norm of 65536 rows of 768 83, 76; 8-bit norm of 121800
+// of 1024 162, 148; rotary of 65536 x 24 heads x 64 83, 79; below it, rotary of 16382 x 20 x 128 (168 MB) 37.4, 39.2.
+constexpr int64_t kLastLevelCache = int64_t(256) << 20;
+
 // ---- over the lanes of a wave.  Lane permutations inside 16 lanes are operands of the vector ALU:
 //      with the lane's neighbour, its pair's, its quad's and its eight's mirror image.
 template <int CTRL>

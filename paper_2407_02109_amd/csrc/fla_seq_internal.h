@@ -22,6 +22,7 @@ struct NormArgs {
     int D;
     int group;               // channels per scale, 0: one per row
     int weight_f32;
+    int nt;                  // outputs are stored non-temporally (set by the launcher)
     float eps, inv_D;
 };
 hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, int cus, hipStream_t stream);

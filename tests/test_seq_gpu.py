@@ -229,7 +229,8 @@ def _scan_inputs(B, L, D, dt, seed, lam_mean=-3.0):
 # B, L, D, lengths
 SCAN_SHAPES = [(1, 1, 1, None), (64, 1, 200, None), (3, 2, 9, None), (2, 16, 66, [16, 3]), (2, 17, 64, None), (1, 256, 70, None), (2, 31, 70, None), (2, 128, 64, None), (1, 129, 65, None),
                (2, 257, 130, [0, 257]), (4, 300, 66, [1, 128, 129, 300]), (1, 1000, 33, None), (2, 4100, 24, [4100, 2049]),
-               (3, 640, 1001, [640, 1, 333]), (1, 9000, 8, None)]
+               (3, 640, 1001, [640, 1, 333]), (1, 9000, 8, None),
+               (1, 36000, 3, None), (2, 20000, 5, [20000, 11111])]   # chains of more links than one look takes in
 
 
 @pytest.mark.parametrize("h0", [True, False], ids=["h0", "zero"])
@@ -363,3 +364,72 @@ def test_empty_problems():
     x = torch.empty(0, 8, device="cuda")
     dx, dw = S.add_rms_norm_bwd(x, x, w, torch.empty(0, device="cuda"))
     assert dx.shape == (0, 8) and (dw == 0).all()
+
+
+# ---- beyond 2^31 elements ------------------------------------------------------------------------
+
+def _big(*shape):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    return torch.randn(*shape, generator=g, device="cuda", dtype=torch.bfloat16)
+
+
+def test_norm_beyond_2_31_elements():
+    _say("big norm")
+    rows, D = 2900000, 768
+    assert rows * D > 2 ** 31
+    x, w = _big(rows, D), torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    y, s, rstd = S.add_rms_norm_fwd_train(x, w)
+    for sl in (slice(0, 50), slice(rows - 50, rows)):
+        ys, _, rs = S.add_rms_norm_fwd_train(x[sl], w)
+        assert torch.equal(y[sl], ys) and torch.equal(rstd[sl], rs)
+    q, sc, _ = S.add_rms_norm_q8(x, w, group=64)
+    qs, scs, _ = S.add_rms_norm_q8(x[-50:], w, group=64)
+    assert torch.equal(q[-50:].view(torch.uint8), qs.view(torch.uint8)) and torch.equal(sc[-50:], scs)
+    del q, sc
+    dx, _ = S.add_rms_norm_bwd(y, x, w, rstd)
+    assert torch.equal(dx[-50:], S.add_rms_norm_bwd(y[-50:], x[-50:], w, rstd[-50:])[0])
+    del x, y, dx
+    torch.cuda.empty_cache()
+
+
+def test_rotary_beyond_2_31_elements():
+    _say("big rotary")
+    L, hq, hk, d = 300000, 56, 4, 128
+    qk = _big(1, L, hq + hk, d)
+    assert qk.numel() > 2 ** 31
+    freqs, m = S.rotary_freqs(64)
+    pos = torch.arange(L, device="cuda")[None]
+    q, k = S.rotary(qk[:, :, :hq], qk[:, :, hq:], freqs, pos)
+    for sl in (slice(0, 33), slice(L - 33, L)):
+        qs, ks = S.rotary(qk[:, sl, :hq], qk[:, sl, hq:], freqs, pos[:, sl])
+        assert torch.equal(q[:, sl], qs) and torch.equal(k[:, sl], ks)
+    del qk, q, k
+    torch.cuda.empty_cache()
+
+
+def test_scan_beyond_2_31_elements():
+    """Gates that forget to below 2^-126 within a few hundred tokens, so that the last whole tiles alone give the same
+    bits as in the whole sequence (tiles of the backward and forward both begin at multiples of 256)."""
+    _say("big scan")
+    L, D = 2900224, 768
+    assert L * D > 2 ** 31 and L % 256 == 0
+    x, r, i = (_big(1, L, D) for _ in range(3))
+    r.abs_()                                     # a < exp(-8 softplus(1) / 2) < 0.006
+    lam = torch.ones(D, device="cuda")
+    h, last, states = S.gated_scan_fwd_train(x, r, i, lam)
+    t = slice(L - 2048, L)
+    hs, lasts, _ = S.gated_scan_fwd_train(x[:, t], r[:, t], i[:, t], lam)
+    assert torch.equal(h[:, L - 1024:], hs[:, 1024:]) and torch.equal(last, lasts)
+    grads = S.gated_scan_bwd(x, r, i, lam, states, x)
+    t = slice(0, 2048)
+    _, _, st = S.gated_scan_fwd_train(x[:, t], r[:, t], i[:, t], lam)
+    gs = S.gated_scan_bwd(x[:, t], r[:, t], i[:, t], lam, st, x[:, t])
+    for a, b in zip(grads[:3], gs[:3]):
+        assert torch.equal(a[:, :1024], b[:, :1024])
+    t = slice(L - 2048, L)
+    _, _, st = S.gated_scan_fwd_train(x[:, t], r[:, t], i[:, t], lam)
+    gs = S.gated_scan_bwd(x[:, t], r[:, t], i[:, t], lam, st, x[:, t])
+    for a, b in zip(grads[:3], gs[:3]):
+        assert torch.equal(a[:, L - 1024:], b[:, 1024:])
+    del x, r, i, h, grads
+    torch.cuda.empty_cache()
