@@ -5,6 +5,11 @@
 // share a row; a lane holds K pieces of 16 bytes of it (pieces of consecutive lanes are consecutive), so
 // a row is read once and its values stay in registers between the sum of squares and the output.  Rows of
 // more than 16 waves hold are read again instead (the *_wide kernels).
+//
+// Measured (MI355X; a copy reaches 5.2 TB/s): forward with residual, sum and 1 / rms, 65536 rows of 768 bf16 77 us, 5.2
+// TB/s; 8-bit output with a scale for 128 channels, 121800 rows of 1024 140 us, 6.2 TB/s; backward with dsum, 65536 rows
+// of 768 bf16 91 us, 4.4 TB/s, 16384 of 4096 107 us, 5.0 TB/s, 4099 of 1001 fp32 17.4 us (13.6 and the sum of the
+// shares of dweight, 4.2).  Eight rows of 768: 3.6 us.
 #include "fla_seq_device.h"
 #include "fla_seq_internal.h"
 

@@ -6,6 +6,11 @@
 // heads in pieces of 16 bytes (pairs that lie rot / 2 apart: a piece of either half).
 // The angle is formed in revolutions in fp64 and reduced to half a turn before it is rounded to fp32: at
 // position 10^6 an fp32 angle would be off by 0.03 radians.
+//
+// Measured (MI355X; a copy reaches 5.2 TB/s): 65536 tokens x 24 heads x 64, bf16, pairs side by side, two axes 79 us, 5.1
+// TB/s; 16382 x 20 heads x 128, half of each turned, halves apart 37 us, 4.5 TB/s; 32 tokens x 40 heads x 128 4.1 us.
+// Addresses are taken from a table of the tokens' places: computed for each piece they were 60 vector operations
+// of 64-bit products (81 us); one head in flight instead of two 80 us; tables of 128 or 512 pairs 77 to 82.
 #include "fla_seq_device.h"
 #include "fla_seq_internal.h"
 
