@@ -8,7 +8,7 @@
 //
 // Measured (MI355X; a copy reaches 5.2 TB/s): forward with residual, sum and 1 / rms, 65536 rows of 768 bf16 77 us, 5.2
 // TB/s; 8-bit output with a scale for 128 channels, 121800 rows of 1024 140 us, 6.2 TB/s; backward with dsum, 65536 rows
-// of 768 bf16 91 us, 4.4 TB/s, 16384 of 4096 107 us, 5.0 TB/s, 4099 of 1001 fp32 17.4 us (13.6 and the sum of the
+// of 768 bf16 74 us, 5.4 TB/s, 16384 of 4096 100 us, 5.4 TB/s, 4099 of 1001 fp32 17.4 us (13.6 and the sum of the
 // shares of dweight, 4.2).  Eight rows of 768: 3.6 us.
 #include "fla_seq_device.h"
 #include "fla_seq_internal.h"
@@ -274,44 +274,64 @@ __global__ __launch_bounds__(Row<W>::kThreads) void norm_bwd(NormBwdArgs a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) dw[k][j] = 0.f;
     }
-    for (int64_t row = rw.row0(); row < a.rows; row += (int64_t)gridDim.x * Row<W>::kRows) {
+    // A row's pieces as they lie in memory; the next row's are asked for before this one's sum is waited for, where the
+    // registers hold both (65536 rows of 768 bf16 90 -> 73 us; with four pieces of fp32 a lane two waves fewer on a SIMD,
+    // 4099 of 1001 18.9 -> 20.1; 16 waves of two pieces of bf16 spill).
+    constexpr bool AHEAD = K <= 2 && !(W == 16 && K == 2 && sizeof(T) == 2);
+    struct Raw {
+        u32x4_any s[K], dy[K], ds[K];
+        float rstd;
+    };
+    auto ask = [&](Raw& r, int64_t row) {
         const T* sp = static_cast<const T*>(a.s) + row * a.s_stride;
         const T* dyp = static_cast<const T*>(a.dy) + row * a.dy_stride;
-        const float rstd = a.rstd[row];
-        float s[K][N], dy[K][N];
+        const T* dsp = static_cast<const T*>(a.dsum) + (a.dsum ? row * a.dsum_stride : 0);
+        r.rstd = a.rstd[row];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = (k * 64 * W + rw.first) * N;
-            load_piece<NT>(sp + col, a.D - col, s[k]);
-            load_piece<NT>(dyp + col, a.D - col, dy[k]);
+            r.s[k] = load_raw<NT>(sp + col, a.D - col);
+            r.dy[k] = load_raw<NT>(dyp + col, a.D - col);
+            r.ds[k] = a.dsum ? load_raw<NT>(dsp + col, a.D - col) : u32x4_any{0u, 0u, 0u, 0u};
         }
+    };
+    const int64_t step = (int64_t)gridDim.x * Row<W>::kRows;
+    int64_t row = rw.row0();
+    Raw now, next;
+    if (AHEAD && row < a.rows) ask(now, row);
+    for (; row < a.rows; row += step) {
+        if constexpr (!AHEAD)
+            ask(now, row);
+        else if (row + step < a.rows)
+            ask(next, row + step);
         float along = 0.f;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            float s[N], dy[N];
+            unpack(now.s[k], s);
+            unpack(now.dy[k], dy);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                s[k][j] *= rstd;
-                dw[k][j] = __builtin_fmaf(dy[k][j], s[k][j], dw[k][j]);
-                dy[k][j] *= w[k][j];
-                along = __builtin_fmaf(dy[k][j], s[k][j], along);
+                const float v = dy[j] * (s[j] * now.rstd);
+                dw[k][j] += v;
+                along = __builtin_fmaf(v, w[k][j], along);
             }
+        }
         along = row_sum<W>(along, red, buf, rw.wave) * a.inv_D;
         T* dx = static_cast<T*>(a.dx) + row * a.D;
-        const T* ds = a.dsum ? static_cast<const T*>(a.dsum) + row * a.dsum_stride : nullptr;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int col = (k * 64 * W + rw.first) * N;
-            float t[N];
-            if (ds) {
-                load_piece<NT>(ds + col, a.D - col, t);
-            } else {
+            float s[N], dy[N], t[N];
+            unpack(now.s[k], s);
+            unpack(now.dy[k], dy);
+            unpack(now.ds[k], t);
 #pragma unroll
-                for (int j = 0; j < N; ++j) t[j] = 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) t[j] = __builtin_fmaf(__builtin_fmaf(-s[k][j], along, dy[k][j]), rstd, t[j]);
+            for (int j = 0; j < N; ++j)
+                t[j] = __builtin_fmaf(__builtin_fmaf(-(s[j] * now.rstd), along, dy[j] * w[k][j]), now.rstd, t[j]);
             store_piece(dx + col, a.D - col, t);
         }
+        if constexpr (AHEAD) now = next;
     }
     float* out = a.ws + (int64_t)blockIdx.x * a.D;
     if constexpr (W == 1) {
@@ -405,8 +425,8 @@ bool fwd_width(int64_t pieces, F&& f) {
     FLA_WIDTH(16, 4)
     return false;
 }
-// Backward, where a lane keeps four values for each channel: as few pieces of bf16 as the waves allow (with 4 in a
-// lane two waves fit a SIMD: 8192 rows of 2048 43 us, with one and four waves a row 35), up to 4 of fp32.
+// Backward, where a lane keeps more for each channel: as few pieces of bf16 as the waves allow (with 4 in a lane two
+// waves fit a SIMD: 8192 rows of 2048 43 us, with one and four waves a row 35), up to 4 of fp32.
 template <typename T, typename F>
 bool bwd_width(int64_t pieces, F&& f) {
     FLA_WIDTH(1, 1)

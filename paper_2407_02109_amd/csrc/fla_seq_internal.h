@@ -46,10 +46,11 @@ struct NormBwdArgs {
     int lines;               // rows are whole cache lines
 };
 // Workgroups of the backward at most, each with a share of dweight in the workspace: about as many as the chip holds
-// of them (rows of up to 512 channels: a few registers, of more than 4096: 16 waves).  us a call, bf16, for 512 / 1024 /
-// 256: 65536 rows of 768 144, 91, 246; 131072 of 256 147, 88, 261; 4096 of 16384 128, 156, 117.
+// of them.  us a call, bf16, with 768 / 1024 / 2048 of them (131072 of 256: 1024 / 1536 / 2048): 65536 rows of 768 73,
+// 86, 80; 16384 of 4096 100, 105, 104; 131072 of 256 59, 73, 63; of 16 waves, with 256 / 512 / 1024: 4096 of 16384 117,
+// 128, 156.
 inline int norm_bwd_blocks(int64_t rows, int D) {
-    const int most = D <= 512 ? 1536 : D <= 4096 ? 1024 : 256;
+    const int most = D <= 512 ? 1024 : D <= 4096 ? 768 : 256;
     return rows < most ? (int)rows : most;
 }
 hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream);
