@@ -9,6 +9,7 @@ belongs to that stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 from .binding import FlaError, _check, _lock, _ptr, _stream
@@ -96,6 +97,7 @@ def fla_add_rms_norm_q8(x, x_stride, residual, residual_stride, weight, q, scale
         group, eps, dtype, weight_dtype, _stream(stream)), check)
 
 
+@functools.lru_cache(maxsize=1024, typed=True)   # a function of the sizes alone
 def fla_add_rms_norm_bwd_workspace(rows, D) -> int:
     return _size(load_seq_library().fla_add_rms_norm_bwd_workspace, rows, D)
 
@@ -125,14 +127,17 @@ def fla_rotary(q, q_strides, k, k_strides, q_out, qo_strides, k_out, ko_strides,
         _stream(stream)), check)
 
 
+@functools.lru_cache(maxsize=1024, typed=True)   # a function of the sizes alone
 def fla_gated_scan_states(B, L, D) -> int:
     return _size(load_seq_library().fla_gated_scan_states, B, L, D)
 
 
+@functools.lru_cache(maxsize=1024, typed=True)   # a function of the sizes alone
 def fla_gated_scan_workspace(B, L, D) -> int:
     return _size(load_seq_library().fla_gated_scan_workspace, B, L, D)
 
 
+@functools.lru_cache(maxsize=1024, typed=True)   # a function of the sizes alone
 def fla_gated_scan_bwd_workspace(B, L, D) -> int:
     return _size(load_seq_library().fla_gated_scan_bwd_workspace, B, L, D)
 
@@ -245,34 +250,36 @@ def _strides(name, t):
 
 
 def _norm_args(x, weight, residual):
-    dtype = _dtype(x)
-    stride = _rows("x", x)
-    D = x.shape[-1]
-    rstride = 0
+    dtype = wdtype = _dtype(x)
+    shape = x.shape
+    stride, rstride = _rows("x", x), 0
+    D = shape[-1]
     if residual is not None:
-        _same("residual", residual, x, x.shape)
+        _same("residual", residual, x, shape)
         rstride = _rows("residual", residual)
     if weight.dtype != x.dtype:
         import torch
+        wdtype = FLA_F32
         _whole("weight", weight, x, (D,), torch.float32)
     else:
         _whole("weight", weight, x, (D,))
-    return dtype, _dtype(weight), x.numel() // D if D else 0, D, stride, rstride
+    return dtype, wdtype, x.numel() // D if D else 0, D, stride, rstride
 
 
 def _norm_fwd(x, weight, residual, eps, out, sum_out, keep, stream):
     import torch
     dtype, wdtype, rows, D, stride, rstride = _norm_args(x, weight, residual)
-    for name, t in (("out", out), ("sum_out", sum_out)):
-        if t is not None:
-            _whole(name, t, x, x.shape)
+    if out is not None:
+        _whole("out", out, x, x.shape)
+    if sum_out is not None:
+        _whole("sum_out", sum_out, x, x.shape)
 
     def body(raw):
         y = _new(x) if out is None else out
         s = sum_out
         if s is None and residual is not None:
             s = _new(x)
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if keep else None
+        rstd = x.new_empty(x.shape[:-1], dtype=torch.float32) if keep else None
         _done(load_seq_library().fla_add_rms_norm_fwd(
             x.data_ptr(), stride, _at(residual), rstride, weight.data_ptr(), y.data_ptr(), _at(s), _at(rstd), rows, D, eps,
             dtype, wdtype, raw))
@@ -307,12 +314,14 @@ def add_rms_norm_q8(x, weight, residual=None, eps=1e-6, group=0, sum_out=None, s
         raise ValueError("group must be 0, 32, 64 or 128, got %r" % (group,))
 
     def body(raw):
-        q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-        scales = torch.empty((*x.shape[:-1], -(-D // group) if group else 1), dtype=torch.float32, device=x.device)
+        q = x.new_empty(x.shape, dtype=torch.float8_e4m3fn)
+        scales = x.new_empty((*x.shape[:-1], -(-D // group) if group else 1), dtype=torch.float32)
         s = sum_out
         if s is None and residual is not None:
             s = _new(x)
-        fla_add_rms_norm_q8(x, stride, residual, rstride, weight, q, scales, s, rows, D, group, eps, dtype, wdtype, raw)
+        _done(load_seq_library().fla_add_rms_norm_q8(
+            x.data_ptr(), stride, _at(residual), rstride, weight.data_ptr(), q.data_ptr(), scales.data_ptr(), _at(s), rows,
+            D, group, eps, dtype, wdtype, raw))
         return q, scales, x if s is None else s
 
     return _on(x, stream, body)
@@ -331,11 +340,11 @@ def add_rms_norm_bwd(dy, s, weight, rstd, dsum=None, stream=None):
 
     def body(raw):
         dx = _new(s)
-        dw = torch.empty(D, dtype=torch.float32, device=s.device)
         nbytes = fla_add_rms_norm_bwd_workspace(rows, D)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=s.device)
-        fla_add_rms_norm_bwd(dy, dystride, s, stride, weight, rstd, dsum, dsstride, dx, dw, ws, nbytes, rows, D, dtype,
-                             wdtype, raw)
+        dw, ws = rstd.new_empty(D), rstd.new_empty(nbytes // 4)
+        _done(load_seq_library().fla_add_rms_norm_bwd(
+            dy.data_ptr(), dystride, s.data_ptr(), stride, weight.data_ptr(), rstd.data_ptr(), _at(dsum), dsstride,
+            dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), nbytes, rows, D, dtype, wdtype, raw))
         return dx, dw
 
     return _on(s, stream, body)
@@ -444,11 +453,13 @@ def _scan_fwd(x, r, i, lam, h0, lengths, c, out, keep, stream):
 
     def body(raw):
         h = _new(x) if out is None else out
-        last = torch.empty((B, D), dtype=torch.float32, device=x.device)
-        states = torch.empty(fla_gated_scan_states(B, L, D) // 4, dtype=torch.float32, device=x.device) if keep else None
+        last = lam.new_empty((B, D))
+        states = lam.new_empty(fla_gated_scan_states(B, L, D) // 4) if keep else None
         nbytes = fla_gated_scan_workspace(B, L, D)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
-        fla_gated_scan_fwd(x, xs, r, rs, i, is_, lam, h0, lengths, h, last, states, ws, nbytes, B, L, D, c, dtype, raw)
+        ws = lam.new_empty(nbytes // 4) if nbytes else None
+        _done(load_seq_library().fla_gated_scan_fwd(
+            x.data_ptr(), *xs, r.data_ptr(), *rs, i.data_ptr(), *is_, lam.data_ptr(), _at(h0), _at(lengths), h.data_ptr(),
+            last.data_ptr(), _at(states), _at(ws), nbytes, B, L, D, c, dtype, raw))
         return h, last, states
 
     return _on(x, stream, body)
@@ -509,12 +520,12 @@ def gated_scan_bwd(x, r, i, lam, states, dh, d_last=None, lengths=None, c=8.0, s
 
     def body(raw):
         dx, dr, di = _new(x), _new(x), _new(x)
-        dlam = torch.empty(D, dtype=torch.float32, device=x.device)
-        dh0 = torch.empty((B, D), dtype=torch.float32, device=x.device)
         nbytes = fla_gated_scan_bwd_workspace(B, L, D)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-        fla_gated_scan_bwd(x, xs, r, rs, i, is_, lam, states, lengths, dh, ds, d_last, dx, dr, di, dlam, dh0, ws,
-                           nbytes, B, L, D, c, dtype, raw)
+        dlam, dh0, ws = lam.new_empty(D), lam.new_empty((B, D)), lam.new_empty(nbytes // 4)
+        _done(load_seq_library().fla_gated_scan_bwd(
+            x.data_ptr(), *xs, r.data_ptr(), *rs, i.data_ptr(), *is_, lam.data_ptr(), states.data_ptr(), _at(lengths),
+            _at(dh), *ds, _at(d_last), dx.data_ptr(), dr.data_ptr(), di.data_ptr(), dlam.data_ptr(), dh0.data_ptr(),
+            ws.data_ptr(), nbytes, B, L, D, c, dtype, raw))
         return dx, dr, di, dlam, dh0
 
     return _on(x, stream, body)
