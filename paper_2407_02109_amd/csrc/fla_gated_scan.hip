@@ -20,13 +20,13 @@
 // Workgroups draw the chunks of a column in order, so a workgroup waits only for ones that have begun, and the first
 // of a column waits for none: every wait ends.
 //
-// Measured (MI355X), 65536 tokens x 768 channels, bf16: forward 95 to 100 us, 4.0 to 4.2 TB/s where a copy of that size
+// Measured (MI355X), 65536 tokens x 768 channels, bf16: forward 96 to 102 us, 3.9 to 4.2 TB/s where a copy of that size
 // reaches 5.2; without waiting for the chain it took 82.  A tile's rows come after about 7 us, its state 4 us later
 // (three round trips to words of another XCD, each 1 to 2 us while the memory is busy), during which nothing of it
 // loads; asking for the next tile's rows before the wait (a workgroup staying for several tiles) took 48 registers
 // and was slower, 143 us.  Every word read bypasses the L2s and costs as a memory access: reading 8 links on suspicion
 // with the marks took 139 us instead of 107.  Backward, 2 x 16384 tokens x 1024 channels: 129 to 137 us, 3.4 to 3.6
-// TB/s; 11 us of it the chain, 14 to 20 the arithmetic (78 vector operations a value, eight of them transcendental)
+// TB/s; 11 us of it the chain, 14 to 20 the arithmetic (76 vector operations a value, eight of them transcendental)
 // that two workgroups on a compute unit do not hide, 10 the rows of 128 bytes (of 256 bytes a copy of the
 // same tensors takes 88 us instead of 97).
 #include "fla_seq_device.h"

@@ -8,8 +8,8 @@
 //
 // Measured (MI355X; a copy reaches 5.2 TB/s): forward with residual, sum and 1 / rms, 65536 rows of 768 bf16 77 us, 5.2
 // TB/s; 8-bit output with a scale for 128 channels, 121800 rows of 1024 140 us, 6.2 TB/s; backward with dsum, 65536 rows
-// of 768 bf16 74 us, 5.4 TB/s, 16384 of 4096 100 us, 5.4 TB/s, 4099 of 1001 fp32 17.4 us (13.6 and the sum of the
-// shares of dweight, 4.2).  Eight rows of 768: 3.6 us.
+// of 768 bf16 74 us, 5.4 TB/s, 16384 of 4096 100 us, 5.4 TB/s, 4099 of 1001 fp32 16.5 us (12.4 and the sum of the
+// shares of dweight, 4.0).  Eight rows of 768: 3.6 us.
 #include "fla_seq_device.h"
 #include "fla_seq_internal.h"
 
